@@ -172,9 +172,8 @@ def run(state):
     if own:
         from paper_2608_29748_amd import ops
         if st["op"] == "append":
-            ops.kv_append(st["cache"], st["k"], st["v"], st["kv_len"], row_start=st["row_start"],
-                          max_rows=st["max_rows"], q=st["q"], q_out=st["q_out"], rope=st["rope"],
-                          q_norm=st["q_norm"], k_norm=st["k_norm"], eps=EPS)
+            ops.kv_append(st["cache"], st["k"], st["v"], st["kv_len"], row_start=st["row_start"], q=st["q"],
+                          q_out=st["q_out"], rope=st["rope"], q_norm=st["q_norm"], k_norm=st["k_norm"], eps=EPS)
             return st["q_out"], st["kp"], st["vp"]
         if st["op"] == "window":
             return ops.window_attention(st["cache"], st["q"], st["kv_len"], st["window"], st["sinks"],
