@@ -198,6 +198,102 @@ int rt_destroy(rt_model* m);
 /* Message for the last non-zero status returned on this thread. */
 const char* rt_last_error(void);
 
+/* ---- operators over a paged KV cache ------------------------------------------- */
+
+/* The steps of a round that touch the KV cache, as calls of their own on caches, queries and
+ * outputs of the caller; they need no model.  Each call only enqueues its kernels on hip_stream
+ * (a hipStream_t of the current device; NULL = default stream), allocates nothing, keeps nothing
+ * for later calls and may be captured into a HIP graph; every pointer but the argument
+ * structures' own is device memory.  Results do not depend on other calls, and the same call
+ * repeated gives the same bits.
+ *
+ * The cache: K pages [page][n_kv_heads][16][head_dim] and V pages [page][n_kv_heads][head_dim][16]
+ * of `dtype`, and a page table [n_seqs][max_pages] whose entry j holds the page of a sequence's
+ * positions 16 j .. 16 j + 15.  head_dim is 64 or 128.  Entries of pages that no row reads or
+ * writes may hold anything; an entry outside [0, n_pages) stands for a page without keys: nothing is
+ * written there and no row sees its positions. */
+typedef struct rt_paged_kv {
+  void* k;
+  void* v;
+  const int32_t* page_table;
+  int32_t n_pages, max_pages, n_kv_heads, head_dim, page_size, dtype;
+} rt_paged_kv;
+
+/* The rows of a call.  n_rows rows of n_seqs sequences lie one after the other: those of
+ * sequence s are row_start[s] .. row_start[s + 1] - 1 (row_start: device, n_seqs + 1 offsets that
+ * do not decrease; NULL: every sequence has n_rows / n_seqs rows; sequences without rows are
+ * allowed, and rows from row_start[n_seqs] on are left as they are).  kv_len[s] (device) counts the
+ * keys of sequence s, its rows' own among them: row i of its n rows is at position
+ * kv_len[s] - n + i.  The same kv_len serves rt_kv_append and the attention after it.
+ * Row strides ld* are in elements; rows are 16-byte aligned, and head h of a row is its columns
+ * h * head_dim .. */
+
+/* Appends the rows' keys and values to the cache, and rotates the rows' queries.  Keys (and
+ * queries) first take a per-head RMSNorm where weights [head_dim] of the cache's dtype are given,
+ * then the rotation of their first rot_dim elements, element j with element j + rot_dim / 2:
+ *   y_j = x_j cos - x_{j + rot_dim/2} sin,  y_{j + rot_dim/2} = x_{j + rot_dim/2} cos + x_j sin
+ * with the factors of the row's position from `rope`, fp32 [cos, sin][rope_positions][rot_dim / 2]
+ * (NULL: no rotation).  Everything is computed in fp32 and rounded once.
+ * Rows at positions below 0 or past the page table are skipped, their queries too.  Two rows for
+ * one place of the cache leave either there.  q may be NULL (no queries); q_out may be q itself
+ * where the dtypes and strides agree, and overlaps the inputs in no other way. */
+typedef struct rt_append_args {
+  const void* q;
+  const void* k;
+  const void* v;
+  int64_t ldq, ldk, ldv;
+  void* q_out;             /* the cache's dtype */
+  int64_t ldqo;
+  const int32_t* row_start;
+  const int32_t* kv_len;
+  const float* rope;
+  const void* q_norm;
+  const void* k_norm;
+  int32_t src_dtype;       /* of q, k and v: the cache's dtype or RT_F32 */
+  int32_t n_seqs, n_rows, n_q_heads;
+  int32_t rope_positions;  /* at least 16 * max_pages */
+  int32_t rot_dim;         /* a multiple of 16 up to head_dim */
+  float eps;               /* of the norms */
+} rt_append_args;
+int rt_kv_append(const rt_paged_kv* kv, const rt_append_args* args, void* hip_stream);
+
+/* Grouped-query attention of the rows over the cache: query head h reads KV head
+ * h / (n_q_heads / n_kv_heads).  Sums and softmax statistics are fp32; rows that see no key give
+ * zeros.  What lies in places of the cache that a row does not see, infinities and NaN included,
+ * does not reach its output.
+ *
+ * rt_window_attention: the row at position p sees the keys j <= p with j > p - window (the
+ * window, its own position included) or j < sinks (the first tokens, which stay visible).
+ *
+ * rt_prefix_attention: the row at position p sees every key j <= p, and the positions
+ * 0 .. prefix_len - 1 (a multiple of 16; 0: none) lie in the same pages for every sequence: they are
+ * read once for the whole batch, through the first sequence's page table.
+ *
+ * max_rows and max_kv: the most rows and keys of a sequence, as far as the host knows (0: unknown).
+ * They only size the split of the work: they must be the same for the call and for its workspace,
+ * results are right whatever they say. */
+typedef struct rt_attn_args {
+  const void* q;           /* the cache's dtype */
+  int64_t ldq;
+  void* out;               /* the cache's dtype; does not overlap q */
+  int64_t ldo;
+  const int32_t* row_start;
+  const int32_t* kv_len;
+  int32_t n_seqs, n_rows, n_q_heads, max_rows, max_kv;
+  int32_t window, sinks;   /* rt_window_attention (0 elsewhere) */
+  int32_t prefix_len;      /* rt_prefix_attention (0 elsewhere) */
+  float scale;             /* of the scores; 0: 1 / sqrt(head_dim) */
+} rt_attn_args;
+/* Bytes of device workspace (256-byte aligned) that a call with these arguments needs, from the
+ * counts alone: q and out may be NULL.  0 where it needs none, and for invalid arguments (see
+ * rt_last_error).  Calls that may run at the same time, two captured graphs for instance, need a
+ * workspace each. */
+size_t rt_attn_workspace_bytes(const rt_paged_kv* kv, const rt_attn_args* args);
+int rt_window_attention(const rt_paged_kv* kv, const rt_attn_args* args, void* d_workspace, size_t ws_bytes,
+                        void* hip_stream);
+int rt_prefix_attention(const rt_paged_kv* kv, const rt_attn_args* args, void* d_workspace, size_t ws_bytes,
+                        void* hip_stream);
+
 /* ---- measurement --------------------------------------------------------------- */
 
 /* Launch classes reported by rt_profile_round (one per role in the round). */

@@ -47,7 +47,8 @@ RT_PROF_STAGES = 7
 EXPORTS = ["rt_workspace_bytes", "rt_weight_count", "rt_init_models", "rt_prefill", "rt_spec_round",
            "rt_destroy", "rt_last_error", "rt_set_debug", "rt_spec_round_forced", "rt_debug_read",
            "rt_debug_write", "rt_profile_round", "rt_time_kernel", "rt_ar_steps", "rt_debug_read_rows",
-           "rt_spec_round_static", "rt_stream_read", "rt_weight_elements", "rt_debug_choice"]
+           "rt_spec_round_static", "rt_stream_read", "rt_weight_elements", "rt_debug_choice",
+           "rt_kv_append", "rt_attn_workspace_bytes", "rt_window_attention", "rt_prefix_attention"]
 
 
 class RetraceError(RuntimeError):
@@ -71,6 +72,27 @@ class rt_config(C.Structure):
 class rt_kernel_stat(C.Structure):
     _fields_ = [("kind", C.c_int32), ("launches", C.c_int32), ("ms", C.c_double), ("bytes", C.c_double),
                 ("flops", C.c_double)]
+
+
+class rt_paged_kv(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_table", C.c_void_p), ("n_pages", C.c_int32),
+                ("max_pages", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_size", C.c_int32), ("dtype", C.c_int32)]
+
+
+class rt_append_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("ldq", C.c_int64), ("ldk", C.c_int64),
+                ("ldv", C.c_int64), ("q_out", C.c_void_p), ("ldqo", C.c_int64), ("row_start", C.c_void_p),
+                ("kv_len", C.c_void_p), ("rope", C.c_void_p), ("q_norm", C.c_void_p), ("k_norm", C.c_void_p),
+                ("src_dtype", C.c_int32), ("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("n_q_heads", C.c_int32),
+                ("rope_positions", C.c_int32), ("rot_dim", C.c_int32), ("eps", C.c_float)]
+
+
+class rt_attn_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("ldq", C.c_int64), ("out", C.c_void_p), ("ldo", C.c_int64),
+                ("row_start", C.c_void_p), ("kv_len", C.c_void_p), ("n_seqs", C.c_int32), ("n_rows", C.c_int32),
+                ("n_q_heads", C.c_int32), ("max_rows", C.c_int32), ("max_kv", C.c_int32), ("window", C.c_int32),
+                ("sinks", C.c_int32), ("prefix_len", C.c_int32), ("scale", C.c_float)]
 
 
 def load_library(path: str = LIB_PATH) -> C.CDLL:
@@ -112,10 +134,17 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.rt_time_kernel.argtypes = [P, C.c_int32, C.c_int32, C.POINTER(rt_kernel_stat)]
     lib.rt_ar_steps.argtypes = [P, C.c_int32, i32p, i32p]
     lib.rt_debug_choice.argtypes = [C.POINTER(rt_config), C.c_int32, C.c_int32, C.c_int32]
+    kvp, atp = C.POINTER(rt_paged_kv), C.POINTER(rt_attn_args)
+    lib.rt_kv_append.argtypes = [kvp, C.POINTER(rt_append_args), P]
+    lib.rt_attn_workspace_bytes.argtypes = [kvp, atp]
+    lib.rt_attn_workspace_bytes.restype = C.c_size_t
+    lib.rt_window_attention.argtypes = [kvp, atp, P, C.c_size_t, P]
+    lib.rt_prefix_attention.argtypes = [kvp, atp, P, C.c_size_t, P]
     for name in ("rt_init_models", "rt_prefill", "rt_spec_round", "rt_spec_round_forced", "rt_spec_round_static",
                  "rt_stream_read", "rt_destroy",
                  "rt_set_debug", "rt_debug_read", "rt_debug_read_rows", "rt_debug_write", "rt_profile_round",
-                 "rt_time_kernel", "rt_ar_steps", "rt_debug_choice"):
+                 "rt_time_kernel", "rt_ar_steps", "rt_debug_choice", "rt_kv_append", "rt_window_attention",
+                 "rt_prefix_attention"):
         getattr(lib, name).restype = C.c_int
     return lib
 
@@ -243,6 +272,24 @@ def rt_stream_read(ptr: int, buf_bytes: int, nbytes: int, grid: int, reps: int, 
     us = C.c_double()
     _check(_lib.rt_stream_read(C.c_void_p(ptr), buf_bytes, nbytes, grid, reps, C.c_void_p(stream_ptr), C.byref(us)))
     return us.value
+
+
+def rt_kv_append(kv: rt_paged_kv, args: rt_append_args, stream_ptr: int = 0) -> None:
+    _check(_lib.rt_kv_append(kv, args, stream_ptr))
+
+
+def rt_attn_workspace_bytes(kv: rt_paged_kv, args: rt_attn_args) -> int:
+    return _lib.rt_attn_workspace_bytes(kv, args)
+
+
+def rt_window_attention(kv: rt_paged_kv, args: rt_attn_args, ws_ptr: int = 0, ws_bytes: int = 0,
+                        stream_ptr: int = 0) -> None:
+    _check(_lib.rt_window_attention(kv, args, ws_ptr, ws_bytes, stream_ptr))
+
+
+def rt_prefix_attention(kv: rt_paged_kv, args: rt_attn_args, ws_ptr: int = 0, ws_bytes: int = 0,
+                        stream_ptr: int = 0) -> None:
+    _check(_lib.rt_prefix_attention(kv, args, ws_ptr, ws_bytes, stream_ptr))
 
 
 def rt_set_debug(h: int, flags: int) -> None:

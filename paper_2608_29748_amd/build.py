@@ -11,13 +11,15 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libretrace.so")
 BUILD = os.path.join(HERE, "_build")
-SOURCES = ["gemm.hip", "gemm_mid.hip", "attn.hip", "misc.hip", "sample.hip", "engine.hip", "validate.cpp"]
+SOURCES = ["gemm.hip", "gemm_mid.hip", "attn.hip", "misc.hip", "sample.hip", "paged_append.hip", "paged_attn.hip",
+           "paged_api.hip", "engine.hip", "validate.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed fp32 vector ops stay off: hipcc otherwise forms them from float code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # per-source extras: attention keeps its MFMA accumulators in ordinary VGPRs (the online
 # softmax rescales them with vector ALU ops; accumulation registers would be copied)
-EXTRA = {"attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+EXTRA = {"attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+         "paged_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def _hipcc() -> str:

@@ -1,0 +1,377 @@
+"""The paged-cache operators against plain 64-bit forms (tests/paged_ref.py, with the bounds of
+every comparison): sizes around pages, steps and tiles, ragged rows, strides, windows and sinks,
+shared prefixes, places that no row sees, graphs and streams."""
+import math
+
+import pytest
+import torch
+
+from paged_ref import PAGE, Case, ref_append, ref_attention
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_2608_29748_amd import ops
+    return ops
+
+
+def device(ops, c):
+    t = c.to(DEV)
+    return ops.PagedKV(t["k"], t["v"], t["table"]), t
+
+
+def check(out, ref, tol, what=""):
+    out = out.double().cpu()
+    same = (out == ref) | (torch.isnan(out) & torch.isnan(ref)) | ((out - ref).abs() <= tol)
+    bad = ~same & torch.isfinite(tol) | (torch.isnan(ref) & ~torch.isnan(out) & torch.isfinite(tol))
+    assert not bad.any(), (what, int(bad.sum()), [(i, out[tuple(i)].item(), ref[tuple(i)].item(), tol[tuple(i)].item())
+                                                 for i in torch.nonzero(bad)[:4].tolist()])
+
+
+def attend(ops, c, window=0, sinks=0, prefix=None, out=None, **kw):
+    cache, t = device(ops, c)
+    kw.setdefault("max_rows", max(c.rows))
+    if prefix is None:
+        return ops.window_attention(cache, t["q"], t["kv_len"], window, sinks, row_start=t["start"], out=out, **kw)
+    return ops.prefix_attention(cache, t["q"], t["kv_len"], prefix, row_start=t["start"], out=out, **kw)
+
+
+# ------------------------------------------------------------------ append
+
+@pytest.mark.parametrize("dtype,src", [(BF, BF), (BF, F32), (F32, F32)], ids=["bf16", "bf16-f32", "f32"])
+@pytest.mark.parametrize("hd,rot,norm", [(128, 128, True), (64, 64, False), (128, 32, True), (64, 16, False),
+                                         (64, 0, True), (128, 96, False)])
+def test_append(ops, dtype, src, hd, rot, norm):
+    rows, keys = [1, 0, 16, 33, 5, 40], [1, 7, 16, 50, 21, 90]
+    c = Case(rows, keys, (6, 2, hd), dtype, seed=hd + rot, extra_rows=3)
+    g = torch.Generator().manual_seed(1)
+    qkv = torch.randn(c.n, 6 + 2 * 2, hd, generator=g).to(src)
+    q, k, v = qkv[:, :6], qkv[:, 6:8], qkv[:, 8:]
+    qn = kn = None
+    if norm:
+        qn, kn = (1 + torch.randn(2, hd, generator=g) / 8).to(dtype)
+    rope = ops.rope_table(1e4, rot, c.width * PAGE + 5, "cpu") if rot else None
+    (qo, qt), (kp, kt), (vp, vt) = ref_append(c, q, k, v, rope, rot, qn, kn)
+    cache, t = device(ops, c)
+    d = qkv.to(DEV)
+    gpu = lambda x: None if x is None else x.to(DEV)   # noqa: E731
+    out = torch.full((c.n, 6, hd), 7.0, dtype=dtype, device=DEV)
+    got = ops.kv_append(cache, d[:, 6:8], d[:, 8:], t["kv_len"], row_start=t["start"], q=d[:, :6], q_out=out,
+                        rope=gpu(rope), q_norm=gpu(qn), k_norm=gpu(kn))
+    assert got is out
+    check(got, qo, qt, "q")
+    check(cache.k, kp, kt, "k")
+    check(cache.v, vp, vt, "v")
+    assert (out[-3:] == 7).all()              # rows behind the last sequence
+
+
+@pytest.mark.parametrize("heads", [(1, 1, 64), (40, 8, 128), (9, 3, 64)])
+def test_append_uniform_without_queries_and_in_place(ops, heads):
+    hq, hkv, hd = heads
+    c = Case([3, 3, 3], [3, 18, 40], heads, BF, ragged=False)
+    g = torch.Generator().manual_seed(2)
+    q, k, v = (torch.randn(9, h, hd, generator=g).to(BF) for h in (hq, hkv, hkv))
+    rope = ops.rope_table(1e6, hd, c.width * PAGE, "cpu")
+    (qo, qt), (kp, kt), (vp, vt) = ref_append(c, q, k, v, rope, hd)
+    cache, t = device(ops, c)
+    assert ops.kv_append(cache, k.to(DEV), v.to(DEV), t["kv_len"], rope=rope.to(DEV)) is None
+    check(cache.k, kp, kt, "k")
+    check(cache.v, vp, vt, "v")
+    d = q.to(DEV)
+    ops.kv_append(cache, k.to(DEV), v.to(DEV), t["kv_len"], rope=rope.to(DEV), q=d, q_out=d)
+    check(d, qo, qt, "q in place")
+    check(cache.k, kp, kt, "k again")
+
+
+def test_append_skips_what_has_no_place(ops):
+    """Positions below 0 and past the table, and pages outside the pool."""
+    c = Case([4, 4, 2], [2, 34, 18], (2, 2, 64), F32, max_pages=2, extra_pages=2)
+    c.table[2, 1] = c.n_pages                 # the rows of sequence 2 (16, 17) have no page
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (torch.randn(10, 2, 64, generator=g) for _ in range(3))
+    (qo, qt), (kp, kt), (vp, vt) = ref_append(c, q, k, v)
+    cache, t = device(ops, c)
+    out = torch.full((10, 2, 64), 7.0, device=DEV)
+    ops.kv_append(cache, k.to(DEV), v.to(DEV), t["kv_len"], row_start=t["start"], q=q.to(DEV), q_out=out)
+    check(out, qo.nan_to_num(7.0), torch.where(torch.isnan(qo), 0.0, qt), "q")
+    check(cache.k, kp, kt, "k")
+    check(cache.v, vp, vt, "v")
+
+
+# ------------------------------------------------------------------ window attention
+
+LENS = [1, 2, 15, 16, 17, 31, 32, 33, 47, 63, 64, 65, 127, 128, 129, 257, 1000]
+
+
+@pytest.mark.parametrize("heads,dtype", [((4, 2, 64), F32), ((4, 4, 128), F32), ((8, 2, 64), BF), ((40, 8, 128), BF),
+                                         ((3, 1, 128), BF)], ids=repr)
+@pytest.mark.parametrize("window,sinks", [(1, 0), (16, 1), (33, 4), (100, 40), (5000, 3)])
+def test_window_steps(ops, heads, dtype, window, sinks):
+    c = Case([1] * len(LENS), LENS, heads, dtype, seed=window, ragged=False)
+    check(attend(ops, c, window, sinks, max_kv=1000), *ref_attention(c, window, sinks))
+
+
+RAGGED = [([1, 0, 5, 33, 0, 70, 2], [1, 4, 5, 40, 9, 300, 150]), ([130], [130]), ([17, 64, 1], [200, 64, 33]),
+          ([0, 0, 1], [3, 0, 0]), ([6, 9], [3, 4]), ([257, 40], [700, 40])]
+
+
+@pytest.mark.parametrize("heads,dtype", [((4, 2, 64), F32), ((2, 1, 128), F32), ((10, 2, 64), BF), ((4, 1, 128), BF),
+                                         ((6, 2, 128), BF), ((32, 2, 64), BF)], ids=repr)
+@pytest.mark.parametrize("window,sinks", [(7, 2), (64, 0), (96, 33), (100000, 0)])
+@pytest.mark.parametrize("shape", range(len(RAGGED)))
+def test_window_prompts(ops, heads, dtype, window, sinks, shape):
+    rows, keys = RAGGED[shape]
+    c = Case(rows, keys, heads, dtype, seed=shape, extra_rows=2, q_pad=16)
+    out = torch.full((c.n, c.hq * c.hd + 24), 7.0, dtype=dtype, device=DEV)
+    view = out[:, :c.hq * c.hd].unflatten(1, (c.hq, c.hd))
+    ref, tol = ref_attention(c, window, sinks)
+    assert attend(ops, c, window, sinks, out=view) is view
+    check(view, ref, tol)
+    assert (out[-2:] == 7).all() and (out[:, c.hq * c.hd:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 3, 40, 150])
+def test_hints_do_not_change_what_is_seen(ops, dtype, rows):
+    c = Case([rows, rows], [600, 333], (4, 2, 64), dtype, ragged=True)
+    ref, tol = ref_attention(c, 200, 5)
+    for max_rows, max_kv in ((0, 0), (1, 1), (rows, 600), (10 ** 6, 10 ** 6)):
+        check(attend(ops, c, 200, 5, max_rows=max_rows, max_kv=max_kv), ref, tol, (max_rows, max_kv))
+
+
+def test_scale(ops):
+    c = Case([3, 20], [40, 50], (4, 2, 64), F32)
+    check(attend(ops, c, 30, 2, scale=0.03), *ref_attention(c, 30, 2, scale=0.03))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 6, 90])
+@pytest.mark.parametrize("junk", [math.nan, math.inf, -math.inf])
+def test_unseen_places_may_hold_anything(ops, dtype, rows, junk):
+    """Behind the last key, between sinks and window, after a row's own position, in free pages."""
+    window, sinks = 37, 3
+    keys = [200, 131, rows]
+    clean = Case([rows] * 3, keys, (8, 2, 128), dtype, seed=5)
+    ref, tol = ref_attention(clean, window, sinks)
+    c = Case([rows] * 3, keys, (8, 2, 128), dtype, seed=5, fill=junk)
+    for s in range(3):
+        for j in range(sinks, max(sinks, keys[s] - rows - window + 1)):      # seen by no row
+            page, slot = c.place(s, j)
+            c.kp[page, :, slot] = junk
+            c.vp[page, :, :, slot] = junk
+    check(attend(ops, c, window, sinks), ref, tol)
+    # the last key of sequence 0 is seen by its last row alone, a key of its window's edge by the first
+    page, slot = c.place(0, keys[0] - 1)
+    c.kp[page, :, slot, 0] = junk
+    c.vp[page, :, 3, slot] = junk
+    ref, tol = ref_attention(c, window, sinks)
+    got = attend(ops, c, window, sinks)
+    check(got[:rows - 1], ref[:rows - 1], tol[:rows - 1])
+    check(got[rows:], ref[rows:], tol[rows:])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows", [4, 70])
+def test_a_value_that_is_not_finite_reaches_the_rows_that_see_it(ops, dtype, rows):
+    c = Case([rows], [rows], (4, 2, 64), dtype, seed=8)
+    for j, d, x in ((1, 5, math.inf), (2, 9, -math.inf), (rows - 1, 0, math.nan)):
+        page, slot = c.place(0, j)
+        c.vp[page, :, d, slot] = x
+    ref, tol = ref_attention(c, 1000, 0)
+    got = attend(ops, c, 1000, 0).double().cpu()
+    finite = torch.isfinite(ref)
+    assert (torch.isfinite(got) == finite).all()
+    check(torch.where(finite, got, 0.0), torch.where(finite, ref, 0.0), torch.where(finite, tol, 0.0))
+
+
+def test_pages_outside_the_pool_hold_no_keys(ops):
+    for rows in (1, 50):
+        c = Case([rows, rows], [150, 90], (4, 2, 64), BF, seed=3)
+        c.table[0, 0] = -7                     # before the window: never read
+        c.table[0, 8] = c.n_pages + 100        # positions 128 .. 143: no keys
+        c.table[1, 5] = 1 << 30
+        check(attend(ops, c, 60, 0), *ref_attention(c, 60, 0))
+
+
+def test_no_keys_at_all(ops):
+    c = Case([1, 2, 1], [0, 1, -5], (4, 2, 64), BF)
+    got = attend(ops, c, 8, 2)
+    check(got, *ref_attention(c, 8, 2))
+    assert (got[0] == 0).all() and (got[1] == 0).all() and (got[3] == 0).all()
+
+
+def test_more_keys_than_the_table_holds(ops):
+    """kv_len past the page table: the rows see what the table has."""
+    c = Case([1, 4], [40, 45], (4, 2, 64), F32, max_pages=2)
+    check(attend(ops, c, 1000, 0), *ref_attention(c, 1000, 0))
+
+
+def test_edges_of_the_window(ops):
+    """A huge value one place outside of each edge, a weight of about 1/n inside."""
+    for rows, dtype in ((1, BF), (1, F32), (80, BF), (80, F32)):
+        c = Case([rows], [500], (4, 2, 64), dtype, seed=11)
+        c.q_full.zero_()                       # equal weights
+        first = 500 - rows                     # position of row 0
+        for j in (4, first - 64):              # the first place behind the sinks, the last before the window
+            page, slot = c.place(0, j)
+            c.vp[page, :, :, slot] = 1e4
+        ref, tol = ref_attention(c, 64, 4)
+        got = attend(ops, c, 64, 4)
+        check(got, ref, tol)
+        assert got.abs().max() < 100
+
+
+# ------------------------------------------------------------------ prefix attention
+
+@pytest.mark.parametrize("heads,dtype", [((4, 2, 64), F32), ((4, 4, 128), F32), ((8, 2, 64), BF), ((40, 8, 128), BF)],
+                         ids=repr)
+@pytest.mark.parametrize("prefix", [0, 16, 48, 512, 1040])
+@pytest.mark.parametrize("rows", [1, 4])
+def test_prefix_uniform(ops, heads, dtype, prefix, rows):
+    own = [rows, rows + 1, rows + 15, rows + 16, rows + 40, rows + 200, rows]
+    c = Case([rows] * 7, [prefix + x for x in own], heads, dtype, seed=prefix, ragged=False, shared=prefix)
+    check(attend(ops, c, prefix=prefix), *ref_attention(c))
+
+
+@pytest.mark.parametrize("heads,dtype", [((4, 2, 64), F32), ((10, 2, 128), BF), ((3, 3, 64), BF)], ids=repr)
+@pytest.mark.parametrize("prefix", [32, 400])
+def test_prefix_ragged(ops, heads, dtype, prefix):
+    rows, own = [5, 0, 1, 70, 33, 0], [5, 9, 30, 80, 33, 0]
+    c = Case(rows, [prefix + x for x in own], heads, dtype, seed=prefix, extra_rows=3, shared=prefix, q_pad=8)
+    out = torch.full((c.n, c.hq, c.hd), 7.0, dtype=dtype, device=DEV)
+    check(attend(ops, c, prefix=prefix, out=out), *ref_attention(c))
+    assert (out[-3:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_rows_inside_the_prefix(ops, dtype):
+    """Sequences that end within the shared pages see no further than their rows."""
+    c = Case([3, 2, 2, 1], [40, 64, 65, 0], (4, 2, 64), dtype, seed=2, shared=64)
+    for s in range(4):
+        c.table[s, :4] = c.table[1, :4]
+    check(attend(ops, c, prefix=64), *ref_attention(c))
+
+
+@pytest.mark.parametrize("rows", [1, 20])
+def test_prefix_unseen_places(ops, rows):
+    own = [rows, rows + 20]
+    clean = Case([rows] * 2, [96 + x for x in own], (8, 2, 64), BF, seed=6, shared=96)
+    ref, tol = ref_attention(clean)
+    c = Case([rows] * 2, [96 + x for x in own], (8, 2, 64), BF, seed=6, shared=96, fill=math.nan)
+    check(attend(ops, c, prefix=96), ref, tol)
+
+
+def test_many_sequences(ops):
+    """More sequences than a wave has lanes, some without rows."""
+    rows = [i % 3 for i in range(150)]
+    own = [max(r, (7 * i) % 50) for i, r in enumerate(rows)]
+    c = Case(rows, [64 + x for x in own], (4, 2, 64), BF, seed=9, shared=64)
+    check(attend(ops, c, prefix=64), *ref_attention(c))
+    check(attend(ops, c, 40, 3), *ref_attention(c, 40, 3))
+
+
+# ------------------------------------------------------------------ together, and around
+
+def test_far_pages(ops):
+    """Page offsets past 2^31 elements."""
+    hkv, hd, n = 8, 128, (1 << 31) // (8 * 128 * 16) + 64
+    c = Case([2, 40], [100, 90], (16, hkv, hd), BF, seed=4, extra_pages=0)
+    k = torch.empty(n, hkv, PAGE, hd, dtype=BF, device=DEV)
+    v = torch.empty(n, hkv, hd, PAGE, dtype=BF, device=DEV)
+    k[n - c.n_pages:], v[n - c.n_pages:] = c.kp.to(DEV), c.vp.to(DEV)
+    t = c.to(DEV)
+    cache = ops.PagedKV(k, v, torch.where(t["table"] >= 0, t["table"] + (n - c.n_pages), t["table"]))
+    check(ops.window_attention(cache, t["q"], t["kv_len"], 64, 4, row_start=t["start"]), *ref_attention(c, 64, 4))
+    x = torch.randn(42, hkv, hd, generator=torch.Generator().manual_seed(1)).to(BF)
+    _, (kp, kt), (vp, vt) = ref_append(c, None, x, x)
+    ops.kv_append(cache, x.to(DEV), x.to(DEV), t["kv_len"], row_start=t["start"])
+    check(k[n - c.n_pages:], kp, kt)
+    check(v[n - c.n_pages:], vp, vt)
+
+
+def step(ops, cache, t, qkv, rope, prefix, hq, hkv):
+    """One layer's attention of new rows: append, then either attention over the grown cache."""
+    q = ops.kv_append(cache, qkv[:, hq:hq + hkv], qkv[:, hq + hkv:], t["kv_len"], q=qkv[:, :hq], rope=rope)
+    a = ops.window_attention(cache, q, t["kv_len"], 50, 4, max_kv=700)
+    return a, ops.prefix_attention(cache, q, t["kv_len"], prefix, max_kv=700)
+
+
+@pytest.mark.parametrize("dtype,rows", [(BF, 1), (BF, 16), (F32, 1)])
+def test_steps_of_a_batch(ops, dtype, rows):
+    """Rows appended to the cache and attended to, three steps one after the other."""
+    hq, hkv, hd, prefix = 8, 2, 128, 512
+    S, n = 5, 3
+    final = [prefix + 20 + 31 * s + rows * n for s in range(S)]
+    c = Case([rows] * S, final, (hq, hkv, hd), dtype, seed=12, ragged=False, shared=prefix)
+    cache, t = device(ops, c)
+    rope = ops.rope_table(1e6, hd, c.width * PAGE, "cpu")
+    g = torch.Generator().manual_seed(7)
+    for i in range(n):
+        c.keys = [f - rows * (n - 1 - i) for f in final]
+        t["kv_len"] = torch.tensor(c.keys, dtype=torch.int32, device=DEV)
+        qkv = torch.randn(rows * S, hq + 2 * hkv, hd, generator=g)
+        (qo, qt), (kp, kt), (vp, vt) = ref_append(c, qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:], rope, hd)
+        a, b = step(ops, cache, t, qkv.to(DEV), rope.to(DEV), prefix, hq, hkv)
+        check(cache.k, kp, kt, "k")
+        check(cache.v, vp, vt, "v")
+        # the attention on what was stored
+        c.kp, c.vp = cache.k.cpu(), cache.v.cpu()
+        q = ops.kv_append(cache, qkv[:, hq:hq + hkv].to(DEV), qkv[:, hq + hkv:].to(DEV), t["kv_len"],
+                          q=qkv[:, :hq].to(DEV), rope=rope.to(DEV))
+        check(q, qo, qt, "q")
+        c.q_full = q.reshape(rows * S, -1).cpu()
+        check(a, *ref_attention(c, 50, 4), "window")
+        check(b, *ref_attention(c), "prefix")
+
+
+def test_captured_and_replayed(ops):
+    """Two graphs with a workspace each, replayed with growing lengths between eager calls."""
+    hq, hkv, hd, prefix, S = 8, 2, 64, 256, 6
+    c = Case([1] * S, [prefix + 300 + s for s in range(S)], (hq, hkv, hd), BF, ragged=False, shared=prefix)
+    cache, t = device(ops, c)
+    other = ops.PagedKV(cache.k.clone(), cache.v.clone(), t["table"])
+    rope = ops.rope_table(1e6, hd, c.width * PAGE, DEV)
+    qkv = torch.randn(S, hq + 2 * hkv, hd, device=DEV)
+    step(ops, cache, t, qkv, rope, prefix, hq, hkv)
+    graphs, outs = [], []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(step(ops, cache, t, qkv, rope, prefix, hq, hkv))
+        graphs.append(g)
+    for i in range(4):
+        t["kv_len"].copy_(torch.tensor([prefix + 40 * i + 1 + s for s in range(S)], dtype=torch.int32))
+        qkv.normal_()
+        other.k.copy_(cache.k)
+        other.v.copy_(cache.v)
+        want = step(ops, other, t, qkv, rope, prefix, hq, hkv)
+        for g, out in zip(graphs, outs):
+            g.replay()
+        torch.cuda.synchronize()
+        for out in outs:
+            for a, b in zip(out, want):
+                assert torch.equal(a, b)
+        assert torch.equal(cache.k, other.k) and torch.equal(cache.v, other.v)
+
+
+def test_two_streams_at_once(ops):
+    c = Case([1] * 40, [3000] * 40, (8, 2, 128), BF, ragged=False, seed=1)
+    d = Case([200], [3000], (8, 2, 128), BF, seed=2)
+    (c1, t1), (c2, t2) = device(ops, c), device(ops, d)
+    want = (ops.window_attention(c1, t1["q"], t1["kv_len"], 2000, 4), ops.window_attention(c2, t2["q"], t2["kv_len"], 2000, 4))
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for _ in range(5):
+        with torch.cuda.stream(s1):
+            a = ops.window_attention(c1, t1["q"], t1["kv_len"], 2000, 4)
+        with torch.cuda.stream(s2):
+            b = ops.window_attention(c2, t2["q"], t2["kv_len"], 2000, 4)
+        got.append((a, b))
+    torch.cuda.synchronize()
+    for a, b in got:
+        assert torch.equal(a, want[0]) and torch.equal(b, want[1])
