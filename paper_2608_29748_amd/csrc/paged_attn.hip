@@ -31,30 +31,73 @@ __device__ __forceinline__ RowRange row_range(const PagedAttnArgs& a, bool share
   return RowRange{(int)lo, (int)hi, (int)min((long)a.sinks, lo)};
 }
 
-// Steps of the keys [0, snk) and [lo, hi), those of the sinks first.
+// Steps of STEP keys over the keys [0, snk) and [lo, hi), those of the sinks first.
+template <int STEP>
 struct Steps {
   int n_snk, first, n;
-  __device__ __forceinline__ int key(int i) const { return (i < n_snk ? i : first + (i - n_snk)) * kStep; }
+  __device__ __forceinline__ Steps(int snk, int lo, int hi) {
+    const int last = (hi + STEP - 1) / STEP;
+    first = min(lo / STEP, last);
+    n_snk = min((snk + STEP - 1) / STEP, first);
+    n = n_snk + last - first;
+  }
+  __device__ __forceinline__ int key(int i) const { return (i < n_snk ? i : first + (i - n_snk)) * STEP; }
 };
-__device__ __forceinline__ Steps steps_of(int snk, int lo, int hi) {
-  Steps t;
-  t.first = lo / kStep;
-  const int last = (hi + kStep - 1) / kStep;
-  t.n_snk = min((snk + kStep - 1) / kStep, t.first);
-  if (last <= t.first) t.first = last;
-  t.n = t.n_snk + last - t.first;
-  return t;
+
+// What the row (of the call) tok sees; sr: its sequence, where the block has one.
+__device__ __forceinline__ RowRange lane_range(const PagedAttnArgs& a, bool shared, const SeqRows& sr, int tok) {
+  const PagedRows& r = a.r;
+  SeqRows q = sr;
+  if (shared) {
+    int sq = tok;
+    if (r.row_start) {            // the last sequence that starts at or before the row
+      int b = 0, e = r.n_seqs;
+      while (e - b > 1) {
+        const int m = (b + e) >> 1;
+        if (r.row_start[m] <= tok) b = m; else e = m;
+      }
+      sq = b;
+    } else {
+      sq = tok / r.rows_each;
+    }
+    q = seq_rows(r, sq);
+    if (tok < q.a || tok >= q.a + q.n) return RowRange{0, 0, 0};     // a row of no sequence
+  }
+  return row_range(a, shared, (long)q.keys - q.n + (tok - q.a), q.keys);
+}
+// Sequence and row block of block blk (RB (token, head) rows each); false: none.
+__device__ __forceinline__ bool block_rows(const PagedAttnArgs& a, bool shared, int blk, int rows_per_block, int& s,
+                                           int& rb, SeqRows& sr) {
+  const PagedRows& r = a.r;
+  const int G = r.n_q_heads / r.n_kv_heads;
+  s = 0;
+  rb = blk;
+  sr = SeqRows{0, r.n_rows, 0};
+  if (shared) return true;
+  if (r.row_start) {
+    if (!find_block(r.n_seqs, blk, [&](int i) { return (seq_rows(r, i).n * G + rows_per_block - 1) / rows_per_block; }, s, rb))
+      return false;
+  } else {
+    const int per = (r.rows_each * G + rows_per_block - 1) / rows_per_block;
+    s = blk / per;
+    rb = blk % per;
+  }
+  s = __builtin_amdgcn_readfirstlane(s);
+  rb = __builtin_amdgcn_readfirstlane(rb);
+  sr = seq_rows(r, s);
+  return true;
 }
 
-__device__ __forceinline__ int rows16_min(int v) {
+// Over all lanes, in a scalar register.
+__device__ __forceinline__ int wave_min(int v) {
 #pragma unroll
-  for (int o = 1; o < 16; o <<= 1) v = min(v, __shfl_xor(v, o, 64));
-  return v;
+  for (int o = 1; o < 64; o <<= 1) v = min(v, __shfl_xor(v, o, 64));
+  return __builtin_amdgcn_readfirstlane(v);
 }
-__device__ __forceinline__ int rows16_max(int v) {
+__device__ __forceinline__ int wave_max(int v) {
 #pragma unroll
-  for (int o = 1; o < 16; o <<= 1) v = max(v, __shfl_xor(v, o, 64));
-  return v;
+  for (int o = 1; o < 64; o <<= 1) v = max(v, __shfl_xor(v, o, 64));
+  return __builtin_amdgcn_readfirstlane(v);
 }
 
 // Rows kernel: one workgroup of NW waves per block of 16 NT (token, head) rows, KV head and key
@@ -76,20 +119,9 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, in
   const int kvh = blockIdx.x % r.n_kv_heads, split = blockIdx.x / r.n_kv_heads % splits;
   const int blk = blockIdx.x / (r.n_kv_heads * splits);
   const int G = r.n_q_heads / r.n_kv_heads;
-  int s = 0, rb = blk;
-  SeqRows sr{0, r.n_rows, 0};
-  if (!shared) {
-    if (r.row_start) {
-      if (!find_block(r.n_seqs, blk, [&](int i) { return (seq_rows(r, i).n * G + RB - 1) / RB; }, s, rb)) return;
-    } else {
-      const int per = (r.rows_each * G + RB - 1) / RB;
-      s = blk / per;
-      rb = blk % per;
-    }
-    s = __builtin_amdgcn_readfirstlane(s);
-    rb = __builtin_amdgcn_readfirstlane(rb);
-    sr = seq_rows(r, s);
-  }
+  int s, rb;
+  SeqRows sr;
+  if (!block_rows(a, shared, blk, RB, s, rb, sr)) return;
   const int nrows = sr.n * G, row0 = rb * RB;
   if (row0 >= nrows) return;
 
@@ -101,42 +133,24 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, in
   for (int t = 0; t < NT; ++t) {
     const int rr = min(row0 + t * 16 + c16, nrows - 1);
     const int tok = sr.a + rr / G;
-    SeqRows q = sr;
-    if (shared) {
-      int sq;
-      if (r.row_start) {            // the last sequence that starts at or before the row
-        int b = 0, e = r.n_seqs;
-        while (e - b > 1) {
-          const int m = (b + e) >> 1;
-          if (r.row_start[m] <= tok) b = m; else e = m;
-        }
-        sq = b;
-      } else {
-        sq = tok / r.rows_each;
-      }
-      q = seq_rows(r, sq);
-      if (tok < q.a || tok >= q.a + q.n) q.keys = q.n = 0;     // a row of no sequence
-    }
-    const long pos = (long)q.keys - q.n + (tok - q.a);
-    rg[t] = row_range(a, shared, pos, q.keys);
-    if (shared && q.n == 0) rg[t] = RowRange{0, 0, 0};
+    rg[t] = lane_range(a, shared, sr, tok);
     const T* qp = (const T*)a.q + (size_t)tok * a.ldq + (size_t)(kvh * G + rr % G) * HD;
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks) qf[t][ks].load(qp + ks * 32 + g4 * 8);
-    all_lo = min(all_lo, rows16_min(rg[t].lo));
-    max_lo = max(max_lo, rows16_max(rg[t].lo));
-    all_hi = max(all_hi, rows16_max(rg[t].hi));
-    min_hi = min(min_hi, rows16_min(rg[t].hi));
-    all_snk = max(all_snk, rows16_max(rg[t].snk));
-    min_snk = min(min_snk, rows16_min(rg[t].snk));
+    all_lo = min(all_lo, rg[t].lo);
+    max_lo = max(max_lo, rg[t].lo);
+    all_hi = max(all_hi, rg[t].hi);
+    min_hi = min(min_hi, rg[t].hi);
+    all_snk = max(all_snk, rg[t].snk);
+    min_snk = min(min_snk, rg[t].snk);
   }
-  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
-  max_lo = __builtin_amdgcn_readfirstlane(max_lo);
-  all_hi = __builtin_amdgcn_readfirstlane(all_hi);
-  min_hi = __builtin_amdgcn_readfirstlane(min_hi);
-  all_snk = __builtin_amdgcn_readfirstlane(all_snk);
-  min_snk = __builtin_amdgcn_readfirstlane(min_snk);
-  const Steps st = steps_of(all_snk, all_lo, all_hi);
+  all_lo = wave_min(all_lo);
+  max_lo = wave_max(max_lo);
+  all_hi = wave_max(all_hi);
+  min_hi = wave_min(min_hi);
+  all_snk = wave_max(all_snk);
+  min_snk = wave_min(min_snk);
+  const Steps<kStep> st(all_snk, all_lo, all_hi);
   const int per = (st.n + splits - 1) / splits;
   const int i_end = min(st.n, (split + 1) * per);
 
@@ -307,6 +321,291 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, in
   }
 }
 
+// Tile kernel (bf16, many rows per page): one workgroup of four waves per block of 128 (token,
+// head) rows, KV head and key split.  A wave owns 32 rows, one per column of 32x32x16 MFMAs; chunks of
+// 64 keys (four pages of K, four of V, one of each copied by every wave straight into LDS) pass
+// through two LDS stages, the copies of the next chunk in flight while one is used, one barrier a
+// chunk.  S^T = K Q^T with the K rows of a page taken in the order that swaps bits 2 and 3 of the
+// row, so that a lane's eight scores of a page belong to eight consecutive keys, which is the
+// B operand of O^T = V^T P^T as it stands, and V^T's fragments are contiguous 1 KiB reads.  K rows
+// lie in LDS with their 16-byte pieces permuted by the row (the copies' source addresses are), so
+// that the lanes of a K fragment, a row apart, fall on different banks.
+// Weights are rounded once to bf16 before the product with V and summed as rounded, so that a
+// row's weights still add up to one; half the V products of the rows kernel's two-part weights.
+constexpr int kTileRows = 128;
+constexpr int kChunkT = 64;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+template <int HD>
+__global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a, int shared, int splits, int z0, int zs) {
+  constexpr int ROWB = HD * 2, NP = ROWB / 16, PGB = kPage * ROWB, NLD = PGB / 1024;
+  constexpr int PAGES = kChunkT / kPage, STG = 2 * PAGES * PGB;
+  constexpr int NKS = HD / 16, NDT = HD / 32;
+  constexpr int OPB = ROWB + 16;                       // pitch of a finished row in LDS
+  static_assert(2 * STG >= kTileRows * OPB, "finished rows fit the stages");
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STG];
+  const PagedRows& r = a.r;
+  const int lane = threadIdx.x & 63, g = lane >> 5, c32 = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kvh = blockIdx.x % r.n_kv_heads, split = blockIdx.x / r.n_kv_heads % splits;
+  const int blk = blockIdx.x / (r.n_kv_heads * splits);
+  const int G = r.n_q_heads / r.n_kv_heads;
+  int s, rb;
+  SeqRows sr;
+  if (!block_rows(a, shared, blk, kTileRows, s, rb, sr)) return;
+  const int nrows = sr.n * G, row0 = rb * kTileRows;
+  if (row0 >= nrows) return;
+
+  // the keys that any row of the block sees: its first and last rows span them, except over the
+  // rows of several sequences, whose prefix passes take all of the prefix
+  const int first_tok = sr.a + row0 / G, last_tok = sr.a + (min(nrows, row0 + kTileRows) - 1) / G;
+  const RowRange rf = shared ? RowRange{0, min(a.prefix, r.max_pages * kPage), 0} : lane_range(a, false, sr, first_tok);
+  const RowRange rl = shared ? rf : lane_range(a, false, sr, last_tok);
+  const int all_hi = max(rf.hi, rl.hi);
+  const Steps<kChunkT> st(max(rf.snk, rl.snk), min(rf.lo, rl.lo), all_hi);
+  const int per = (st.n + splits - 1) / splits;
+  const int i_beg = split * per, i_end = min(st.n, i_beg + per);
+
+  // this lane's row
+  const int wrow = row0 + w * 32;
+  const bool live = wrow < nrows;                       // this wave has rows
+  const int rr = min(wrow + c32, nrows - 1);
+  const int tok = sr.a + rr / G, head = kvh * G + rr % G;
+  const RowRange rg = lane_range(a, shared, sr, tok);
+  const int min_hi = wave_min(rg.hi), max_lo = wave_max(rg.lo), min_snk = wave_min(rg.snk);
+  const int max_hi = wave_max(rg.hi), min_lo = wave_min(rg.lo), max_snk = wave_max(rg.snk);
+  Frag<bf16_t> qf[NKS];
+  {
+    const bf16_t* qp = (const bf16_t*)a.q + (size_t)tok * a.ldq + (size_t)head * HD + g * 8;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) qf[ks].load(qp + ks * 16);
+  }
+
+  // source offsets of this wave's copies (LDS slot j * 64 + lane of its page)
+  auto swz = [](int row) { return NP == 16 ? row : row >> 1; };
+  int koff[NLD];
+#pragma unroll
+  for (int j = 0; j < NLD; ++j) {
+    const int sl = j * 64 + lane, row = sl / NP, pc = sl % NP;
+    koff[j] = row * ROWB + (pc ^ swz(row)) * 16;
+  }
+  const_i32_t* pt = (const_i32_t*)(r.page_table + (size_t)s * r.max_pages);
+  const int last_page = max(0, (all_hi - 1) / kPage);
+  struct Pages { int id[PAGES]; };
+  auto pages_at = [&](int i) {
+    Pages p;
+    const int pg = st.key(i) / kPage;
+#pragma unroll
+    for (int u = 0; u < PAGES; ++u) p.id[u] = pt[min(pg + u, last_page)];
+    return p;
+  };
+  auto ok_page = [&](int id) { return id >= 0 && id < r.n_pages; };
+  auto issue = [&](const Pages& p, int stage) {
+    const int id = w == 0 ? p.id[0] : w == 1 ? p.id[1] : w == 2 ? p.id[2] : p.id[3];
+    const size_t at = ((size_t)(ok_page(id) ? id : 0) * r.n_kv_heads + kvh) * PGB;
+    const char* kb = (const char*)r.k + at;
+    const char* vb = (const char*)r.v + at + lane * 16;
+    char* l = smem + stage + w * PGB;
+#pragma unroll
+    for (int j = 0; j < NLD; ++j)
+      __builtin_amdgcn_global_load_lds((const void*)(kb + koff[j]), (lds_void_t*)(l + j * 1024), 16, 0, 0);
+#pragma unroll
+    for (int j = 0; j < NLD; ++j)
+      __builtin_amdgcn_global_load_lds((const void*)(vb + j * 1024), (lds_void_t*)(l + PAGES * PGB + j * 1024), 16, 0, 0);
+  };
+  // read offsets: K fragment ks of the tile's rows, V fragments
+  const int krow = (c32 & 16) * 1 + ((c32 & 4) << 1) + ((c32 & 8) >> 1) + (c32 & 3);   // bits 2 and 3 swapped
+  int kad[NKS];
+#pragma unroll
+  for (int ks = 0; ks < NKS; ++ks)
+    kad[ks] = (krow >> 4) * PGB + (krow & 15) * ROWB + ((2 * ks + g) ^ swz(krow & 15)) * 16;
+  const int vad = PAGES * PGB + c32 * 32 + g * 16;
+
+  const float sl2 = a.scale * 1.4426950408889634f;
+  float mref = kMrefInit, lsum = 0.f;
+  f32x16 o[NDT];
+#pragma unroll
+  for (int d = 0; d < NDT; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+
+  Pages cur, nxt;
+  if (i_beg < i_end) {
+    cur = pages_at(i_beg);
+    issue(cur, 0);
+    nxt = pages_at(min(i_beg + 1, i_end - 1));
+  }
+  int stage = 0;
+  for (int i = i_beg; i < i_end; ++i) {
+    wait_vm<0>();      // this wave's copies of chunk i have landed
+    lds_barrier();     // everyone's have; chunk i-1's stage is free
+    const Pages here = cur;
+    if (i + 1 < i_end) {
+      issue(nxt, stage ^ STG);
+      cur = nxt;
+      nxt = pages_at(min(i + 2, i_end - 1));
+    }
+    const int k0 = st.key(i);
+    const char* sm = smem + stage;
+    stage ^= STG;
+    // (a wave none of whose rows sees the chunk passes it by)
+    if (!live || !((k0 < max_hi && k0 + kChunkT > min_lo) || k0 < max_snk)) continue;
+    f32x16 sc[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[t][e] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(sm + kad[ks] + t * 2 * PGB);
+        sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks].v, sc[t], 0, 0, 0);
+      }
+    bool pages_ok = true;
+#pragma unroll
+    for (int u = 0; u < PAGES; ++u) pages_ok = pages_ok && ok_page(here.id[u]);
+    const bool whole = pages_ok && k0 + kChunkT <= min_hi && (k0 >= max_lo || k0 + kChunkT <= min_snk);
+    unsigned bad = 0;                                   // bit 8 page + e: key 16 page + 8 g + e, see below
+    if (!whole) {
+#pragma unroll
+      for (int x = 0; x < 32; ++x) {
+        const int j = k0 + (x >> 3) * kPage + 8 * g + (x & 7);
+        const bool vis = ok_page(here.id[x >> 3]) && j < rg.hi && (j >= rg.lo || j < rg.snk);
+        sc[x >> 4][x & 15] = vis ? sc[x >> 4][x & 15] : -INFINITY;
+      }
+      // keys with a non-finite V element somewhere: a weight of zero must not meet them in a
+      // product, so where rows differ in what they see they are added one by one
+#pragma unroll 1
+      for (int d = 0; d < NDT; ++d)
+#pragma unroll
+        for (int pg = 0; pg < PAGES; ++pg) {
+          const bf16x8 vf = *reinterpret_cast<const bf16x8*>(sm + vad + pg * PGB + d * 1024);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) bad |= ((vf[e] & 0x7f80) == 0x7f80 ? 1u : 0u) << (8 * pg + e);
+        }
+#pragma unroll
+      for (int x = 1; x < 32; x <<= 1) bad |= (unsigned)__shfl_xor((int)bad, x, 64);
+    }
+    float mx = sc[0][0];
+#pragma unroll
+    for (int x = 1; x < 32; ++x) mx = __builtin_elementwise_maximum(mx, sc[x >> 4][x & 15]);
+    {
+      const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = __builtin_elementwise_maximum(__uint_as_float(h[0]), __uint_as_float(h[1])) * sl2;
+    }
+    if (__ballot(mx > mref + 8.f)) {                    // the reference rises by 2^8 or more, or not at all
+      const float mn = fmaxf(mref, mx), al = __builtin_amdgcn_exp2f(mref - mn);
+#pragma unroll
+      for (int d = 0; d < NDT; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] *= al;
+      lsum *= al;
+      mref = mn;
+    }
+    u32x4 pf[PAGES];                                    // weights of a page's eight keys
+#pragma unroll
+    for (int x = 0; x < 32; x += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[x >> 4][x & 15], sl2, -mref));
+      const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[(x + 1) >> 4][(x + 1) & 15], sl2, -mref));
+      const bf2 pk = {(__bf16)p0, (__bf16)p1}, one = {(__bf16)1.f, (__bf16)1.f};
+      lsum = __builtin_amdgcn_fdot2_f32_bf16(pk, one, lsum, false);
+      pf[x >> 3][x >> 1 & 3] = __builtin_bit_cast(unsigned, pk);
+    }
+    if (!__ballot(bad != 0)) {
+#pragma unroll
+      for (int pg = 0; pg < PAGES; ++pg)
+#pragma unroll
+        for (int d = 0; d < NDT; ++d) {
+          const bf16x8 vf = *reinterpret_cast<const bf16x8*>(sm + vad + pg * PGB + d * 1024);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pf[pg]), o[d], 0, 0, 0);
+        }
+      continue;
+    }
+#pragma unroll
+    for (int pg = 0; pg < PAGES; ++pg) {                // the product without those keys
+      u32x4 keep;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        keep[e] = (bad >> (8 * pg + 2 * e) & 1 ? 0u : 0xffffu) | (bad >> (8 * pg + 2 * e + 1) & 1 ? 0u : 0xffff0000u);
+#pragma unroll
+      for (int d = 0; d < NDT; ++d) {
+        const u32x4 vf = *reinterpret_cast<const u32x4*>(sm + vad + pg * PGB + d * 1024) & keep;
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pf[pg]),
+                                                       o[d], 0, 0, 0);
+      }
+    }
+#pragma unroll 1
+    for (int gg = 0; gg < 2; ++gg) {
+#pragma unroll 1
+      for (unsigned m = __builtin_amdgcn_readlane((int)bad, 32 * gg); m; m &= m - 1) {
+        const int x = __builtin_ctz(m);                 // key 16 (x / 8) + 8 gg + x % 8
+        unsigned u = pf[0][0];
+#pragma unroll
+        for (int y = 1; y < 16; ++y) u = (x >> 1) == y ? pf[y >> 2][y & 3] : u;
+        u = (unsigned)__shfl((int)u, c32 + 32 * gg, 64);
+        const float pj = __uint_as_float(x & 1 ? u & 0xffff0000u : u << 16);
+        const bf16_t* vj = reinterpret_cast<const bf16_t*>(sm + PAGES * PGB + (x >> 3) * PGB) + 8 * gg + (x & 7);
+#pragma unroll
+        for (int d = 0; d < NDT; ++d)
+#pragma unroll
+          for (int y = 0; y < 16; ++y) {
+            const float v = bf16_to_f32(vj[(32 * d + 8 * (y >> 2) + 4 * g + (y & 3)) * kPage]);
+            o[d][y] += pj != 0.f ? pj * v : 0.f;
+          }
+      }
+    }
+  }
+  {
+    const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(lsum), __float_as_uint(lsum), false, false);
+    lsum = __uint_as_float(h[0]) + __uint_as_float(h[1]);
+  }
+  const bool row_ok = wrow + c32 < nrows;
+  if (zs > 1) {
+    if (!row_ok) return;
+    const size_t row = ((size_t)(z0 + split) * r.n_rows + tok) * r.n_q_heads + head;
+    float* op = a.part_o + row * HD;
+#pragma unroll
+    for (int d = 0; d < NDT; ++d)
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        *reinterpret_cast<float4*>(op + d * 32 + 8 * b + 4 * g) =
+            make_float4(o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]);
+    if (g == 0) {
+      a.part_ml[row * 2] = mref;
+      a.part_ml[row * 2 + 1] = lsum;
+    }
+    return;
+  }
+  // finished rows through LDS, so that they leave 16 bytes a lane along the row
+  const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
+  lds_barrier();
+  char* mine = smem + (size_t)w * 32 * OPB;
+#pragma unroll
+  for (int d = 0; d < NDT; ++d)
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      uint2 u;
+      bf16_t h[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[e] = lsum == 0.f ? (bf16_t)0 : f32_to_bf16(o[d][4 * b + e] * inv);
+      u.x = h[0] | (unsigned)h[1] << 16;
+      u.y = h[2] | (unsigned)h[3] << 16;
+      *reinterpret_cast<uint2*>(mine + c32 * OPB + (d * 32 + 8 * b + 4 * g) * 2) = u;
+    }
+  wait_lds();
+  for (int x = lane; x < 32 * NP; x += 64) {
+    const int rl = x / NP, pc = x % NP, rw = wrow + rl;
+    if (rw >= nrows) break;
+    const int tk = sr.a + rw / G, col = (kvh * G + rw % G) * HD + pc * 8;
+    const uint4 u = *reinterpret_cast<const uint4*>(mine + rl * OPB + pc * 16);
+    const size_t at = a.packed ? pa_index(tk, col, (size_t)a.ldo) : (size_t)tk * a.ldo + col;
+    *reinterpret_cast<uint4*>((bf16_t*)a.out + at) = u;
+  }
+}
+
 // Joins the z partial results of every (row, head): one wave each, HD / 64 elements a lane.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a, int zs) {
@@ -351,28 +650,34 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a, int z
 constexpr int kRowsNT = 1;
 constexpr int kRowsNW = 4;
 
-static long rows_blocks(const PagedAttnArgs& a, bool shared, int rb) {
+static long row_blocks(const PagedAttnArgs& a, bool shared, int rb) {
   const PagedRows& r = a.r;
   const int G = r.n_q_heads / r.n_kv_heads;
   if (shared) return ((long)r.n_rows * G + rb - 1) / rb;
   if (r.row_start) return (long)r.n_rows * G / rb + r.n_seqs;
   return (long)r.n_seqs * (((long)r.rows_each * G + rb - 1) / rb);
 }
+// bf16 blocks of more than 16 (token, head) rows take the tile kernel.
+static bool tiled(const PagedAttnArgs& a, bool shared, int elem_bytes) {
+  const PagedRows& r = a.r;
+  return elem_bytes == 2 && (long)(shared ? r.n_rows : a.max_rows) * (r.n_q_heads / r.n_kv_heads) > 16 * kRowsNT;
+}
 
 PagedPlan paged_plan(const PagedAttnArgs& a, int elem_bytes) {
-  (void)elem_bytes;
   const PagedRows& r = a.r;
   PagedPlan p{1, 0};
-  auto pick = [&](long units, long keys) {
-    long s = (512 + units - 1) / units;
-    const long most = keys / (2 * kStep * kRowsNW);
+  auto pick = [&](bool shared, long keys) {
+    const bool t = tiled(a, shared, elem_bytes);
+    const long units = row_blocks(a, shared, t ? kTileRows : 16 * kRowsNT) * r.n_kv_heads;
+    long s = 512 / units;
+    const long most = keys / (t ? 4 * kChunkT : 2 * kStep * kRowsNW);
     if (s > most) s = most;
     return (int)(s < 1 ? 1 : s > 32 ? 32 : s);
   };
   long keys = a.max_kv - a.prefix;
   if (a.window > 0 && keys > (long)a.window + a.sinks + a.max_rows) keys = (long)a.window + a.sinks + a.max_rows;
-  p.splits = pick(rows_blocks(a, false, 16 * kRowsNT) * r.n_kv_heads, keys);
-  if (a.prefix > 0) p.shared = pick(rows_blocks(a, true, 16 * kRowsNT) * r.n_kv_heads, a.prefix);
+  p.splits = pick(false, keys);
+  if (a.prefix > 0) p.shared = pick(true, a.prefix);
   return p;
 }
 
@@ -386,9 +691,16 @@ template <typename T, int HD>
 static hipError_t attention_hd(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
   const PagedRows& r = a.r;
   auto launch = [&](bool shared, int splits, int z0) {
-    const long grid = rows_blocks(a, shared, 16 * kRowsNT) * splits * r.n_kv_heads;
+    const bool t = tiled(a, shared, sizeof(T));
+    const long grid = row_blocks(a, shared, t ? kTileRows : 16 * kRowsNT) * splits * r.n_kv_heads;
     if (grid <= 0) return hipSuccess;
     if (grid > 0x7fffffffl) return hipErrorInvalidValue;
+    if constexpr (sizeof(T) == 2) {
+      if (t) {
+        RT_LAUNCH((paged_tile_kernel<HD>), dim3((unsigned)grid), dim3(256), 0, s, a, shared ? 1 : 0, splits, z0, p.z());
+        return hipGetLastError();
+      }
+    }
     RT_LAUNCH((paged_rows_kernel<T, HD, kRowsNT, kRowsNW>), dim3((unsigned)grid), dim3(64 * kRowsNW), 0, s, a,
               shared ? 1 : 0, splits, z0, p.z());
     return hipGetLastError();
