@@ -65,29 +65,37 @@ __device__ __forceinline__ RowRange lane_range(const PagedAttnArgs& a, bool shar
   }
   return row_range(a, shared, (long)q.keys - q.n + (tok - q.a), q.keys);
 }
-// Sequence and row block of block blk (RB (token, head) rows each); false: none.
-__device__ __forceinline__ bool block_rows(const PagedAttnArgs& a, bool shared, int blk, int rows_per_block, int& s,
-                                           int& rb, SeqRows& sr) {
+// Sequence and row block of block blk, of `per` (token, head) rows each; false: none.  The results
+// are the same for every lane and made scalar, so that page ids come by scalar loads.
+__device__ __forceinline__ bool block_rows(const PagedAttnArgs& a, bool shared, int blk, int per, int& s, int& rb,
+                                           SeqRows& sr) {
   const PagedRows& r = a.r;
   const int G = r.n_q_heads / r.n_kv_heads;
-  s = 0;
-  rb = blk;
-  sr = SeqRows{0, r.n_rows, 0};
-  if (shared) return true;
-  if (r.row_start) {
-    if (!find_block(r.n_seqs, blk, [&](int i) { return (seq_rows(r, i).n * G + rows_per_block - 1) / rows_per_block; }, s, rb))
-      return false;
-  } else {
-    const int per = (r.rows_each * G + rows_per_block - 1) / rows_per_block;
-    s = blk / per;
-    rb = blk % per;
+  int s_ = 0, rb_ = blk;
+  SeqRows q{0, r.n_rows, 0};
+  if (!shared) {
+    if (r.row_start) {
+      if (!find_block(r.n_seqs, blk, [&](int i) { return (seq_rows(r, i).n * G + per - 1) / per; }, s_, rb_)) return false;
+    } else {
+      const int n = (r.rows_each * G + per - 1) / per;
+      s_ = blk / n;
+      rb_ = blk % n;
+    }
+    q = seq_rows(r, __builtin_amdgcn_readfirstlane(s_));
   }
-  s = __builtin_amdgcn_readfirstlane(s);
-  rb = __builtin_amdgcn_readfirstlane(rb);
-  sr = seq_rows(r, s);
+  s = __builtin_amdgcn_readfirstlane(s_);
+  rb = __builtin_amdgcn_readfirstlane(rb_);
+  sr = SeqRows{__builtin_amdgcn_readfirstlane(q.a), __builtin_amdgcn_readfirstlane(q.n),
+               __builtin_amdgcn_readfirstlane(q.keys)};
   return true;
 }
 
+// Page table row of sequence s (the same for every lane), as a pointer for scalar loads.
+__device__ __forceinline__ const_i32_t* table_row(const PagedRows& r, int s) {
+  const uint64_t p = (uint64_t)(r.page_table + (size_t)s * r.max_pages);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)p), hi = __builtin_amdgcn_readfirstlane((uint32_t)(p >> 32));
+  return (const_i32_t*)((uint64_t)hi << 32 | lo);
+}
 // Over all lanes, in a scalar register.
 __device__ __forceinline__ int wave_min(int v) {
 #pragma unroll
@@ -154,7 +162,7 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, in
   const int per = (st.n + splits - 1) / splits;
   const int i_end = min(st.n, (split + 1) * per);
 
-  const_i32_t* pt = (const_i32_t*)(r.page_table + (size_t)s * r.max_pages);
+  const_i32_t* pt = table_row(r, s);
   const int last_page = max(0, (all_hi - 1) / kPage);
   const float sl2 = a.scale * 1.4426950408889634f;
   float mref[NT], lsum[NT];
@@ -338,8 +346,19 @@ typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
+// Wave-wide copies of a page of N KiB at src (the same for every lane) into LDS at dst: copy j brings
+// the 16 bytes at off[j] + j * step of every lane to dst + 1024 j + 16 lane.  Buffer copies: after a
+// global one, which counts as flat, every wait for LDS reads would be a full one.
+template <int N>
+__device__ __forceinline__ void copy_page(const char* src, char* dst, const int (&off)[N], int step) {
+  const __amdgpu_buffer_rsrc_t b = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), 0, N * 1024, 0x00027000);
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (lds_void_t*)(dst + j * 1024), 16, off[j], j * step, 0, 0);
+}
+
 template <int HD>
-__global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a, int shared, int splits, int z0, int zs) {
+__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void paged_tile_kernel(PagedAttnArgs a, int shared, int splits, int z0, int zs) {
   constexpr int ROWB = HD * 2, NP = ROWB / 16, PGB = kPage * ROWB, NLD = PGB / 1024;
   constexpr int PAGES = kChunkT / kPage, STG = 2 * PAGES * PGB;
   constexpr int NKS = HD / 16, NDT = HD / 32;
@@ -363,8 +382,9 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a, int
   const int first_tok = sr.a + row0 / G, last_tok = sr.a + (min(nrows, row0 + kTileRows) - 1) / G;
   const RowRange rf = shared ? RowRange{0, min(a.prefix, r.max_pages * kPage), 0} : lane_range(a, false, sr, first_tok);
   const RowRange rl = shared ? rf : lane_range(a, false, sr, last_tok);
-  const int all_hi = max(rf.hi, rl.hi);
-  const Steps<kChunkT> st(max(rf.snk, rl.snk), min(rf.lo, rl.lo), all_hi);
+  const int all_hi = __builtin_amdgcn_readfirstlane(max(rf.hi, rl.hi));
+  const Steps<kChunkT> st(__builtin_amdgcn_readfirstlane(max(rf.snk, rl.snk)),
+                          __builtin_amdgcn_readfirstlane(min(rf.lo, rl.lo)), all_hi);
   const int per = (st.n + splits - 1) / splits;
   const int i_beg = split * per, i_end = min(st.n, i_beg + per);
 
@@ -385,42 +405,35 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a, int
 
   // source offsets of this wave's copies (LDS slot j * 64 + lane of its page)
   auto swz = [](int row) { return NP == 16 ? row : row >> 1; };
-  int koff[NLD];
+  int koff[NLD], voff[NLD];
 #pragma unroll
   for (int j = 0; j < NLD; ++j) {
     const int sl = j * 64 + lane, row = sl / NP, pc = sl % NP;
     koff[j] = row * ROWB + (pc ^ swz(row)) * 16;
+    voff[j] = lane * 16;
   }
-  const_i32_t* pt = (const_i32_t*)(r.page_table + (size_t)s * r.max_pages);
+  const_i32_t* pt = table_row(r, s);
   const int last_page = max(0, (all_hi - 1) / kPage);
-  struct Pages { int id[PAGES]; };
+  struct Pages { int id[PAGES], own; };              // own: the page that this wave copies
   auto pages_at = [&](int i) {
     Pages p;
     const int pg = st.key(i) / kPage;
 #pragma unroll
     for (int u = 0; u < PAGES; ++u) p.id[u] = pt[min(pg + u, last_page)];
+    p.own = pt[min(pg + w, last_page)];
     return p;
   };
   auto ok_page = [&](int id) { return id >= 0 && id < r.n_pages; };
   auto issue = [&](const Pages& p, int stage) {
-    const int id = w == 0 ? p.id[0] : w == 1 ? p.id[1] : w == 2 ? p.id[2] : p.id[3];
-    const size_t at = ((size_t)(ok_page(id) ? id : 0) * r.n_kv_heads + kvh) * PGB;
-    const char* kb = (const char*)r.k + at;
-    const char* vb = (const char*)r.v + at + lane * 16;
+    const size_t at = ((size_t)(ok_page(p.own) ? p.own : 0) * r.n_kv_heads + kvh) * PGB;
     char* l = smem + stage + w * PGB;
-#pragma unroll
-    for (int j = 0; j < NLD; ++j)
-      __builtin_amdgcn_global_load_lds((const void*)(kb + koff[j]), (lds_void_t*)(l + j * 1024), 16, 0, 0);
-#pragma unroll
-    for (int j = 0; j < NLD; ++j)
-      __builtin_amdgcn_global_load_lds((const void*)(vb + j * 1024), (lds_void_t*)(l + PAGES * PGB + j * 1024), 16, 0, 0);
+    copy_page<NLD>((const char*)r.k + at, l, koff, 0);
+    copy_page<NLD>((const char*)r.v + at, l + PAGES * PGB, voff, 1024);
   };
   // read offsets: K fragment ks of the tile's rows, V fragments
   const int krow = (c32 & 16) * 1 + ((c32 & 4) << 1) + ((c32 & 8) >> 1) + (c32 & 3);   // bits 2 and 3 swapped
-  int kad[NKS];
-#pragma unroll
-  for (int ks = 0; ks < NKS; ++ks)
-    kad[ks] = (krow >> 4) * PGB + (krow & 15) * ROWB + ((2 * ks + g) ^ swz(krow & 15)) * 16;
+  // (piece 2 ks + g of the row, permuted: the pieces of ks differ from those of 0 in bits alone)
+  const int kad = (krow >> 4) * PGB + (krow & 15) * ROWB + (g ^ swz(krow & 15)) * 16;
   const int vad = PAGES * PGB + c32 * 32 + g * 16;
 
   const float sl2 = a.scale * 1.4426950408889634f;
@@ -431,28 +444,49 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a, int
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
 
-  Pages cur, nxt;
+  // page ids of the chunk in use and of the next two: the last are asked for at the end of a
+  // step (a scalar load under way would make every LDS wait a full one)
+  Pages cur{}, nxt{}, far{};
   if (i_beg < i_end) {
     cur = pages_at(i_beg);
     issue(cur, 0);
     nxt = pages_at(min(i_beg + 1, i_end - 1));
+    far = pages_at(min(i_beg + 2, i_end - 1));
   }
   int stage = 0;
   for (int i = i_beg; i < i_end; ++i) {
     wait_vm<0>();      // this wave's copies of chunk i have landed
     lds_barrier();     // everyone's have; chunk i-1's stage is free
     const Pages here = cur;
-    if (i + 1 < i_end) {
-      issue(nxt, stage ^ STG);
-      cur = nxt;
-      nxt = pages_at(min(i + 2, i_end - 1));
-    }
+    if (i + 1 < i_end) issue(nxt, stage ^ STG);
+    cur = nxt;
+    nxt = far;
+    auto next_pages = [&]() { far = pages_at(min(i + 3, i_end - 1)); };
     const int k0 = st.key(i);
     const char* sm = smem + stage;
     stage ^= STG;
     // (a wave none of whose rows sees the chunk passes it by)
-    if (!live || !((k0 < max_hi && k0 + kChunkT > min_lo) || k0 < max_snk)) continue;
+    if (!live || !((k0 < max_hi && k0 + kChunkT > min_lo) || k0 < max_snk)) {
+      next_pages();
+      continue;
+    }
+    // all of the chunk's K fragments are asked for before the first product, and V fragments
+    // before the softmax, whose arithmetic covers their way
     f32x16 sc[2];
+    bf16x8 kf[2][NKS], vf[PAGES][NDT];
+    auto late_v = [&]() {          // (the registers of the scores are free by then)
+#pragma unroll
+      for (int pg = PAGES / 2; pg < PAGES; ++pg)
+#pragma unroll
+        for (int d = 0; d < NDT; ++d) vf[pg][d] = *reinterpret_cast<const bf16x8*>(sm + vad + pg * PGB + d * 1024);
+    };
+    const int ka = (int)(sm - smem) + kad;
+    wait_lds();                    // (the page ids are here: from now on LDS reads alone are waited for)
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) kf[t][ks] = *reinterpret_cast<const bf16x8*>(smem + (ka ^ (32 * ks)) + t * 2 * PGB);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -460,10 +494,13 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a, int
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(sm + kad[ks] + t * 2 * PGB);
-        sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks].v, sc[t], 0, 0, 0);
-      }
+      for (int t = 0; t < 2; ++t)
+        sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t][ks], qf[ks].v, sc[t], 0, 0, 0);
+#pragma unroll
+    for (int pg = 0; pg < PAGES / 2; ++pg)
+#pragma unroll
+      for (int d = 0; d < NDT; ++d) vf[pg][d] = *reinterpret_cast<const bf16x8*>(sm + vad + pg * PGB + d * 1024);
+    __builtin_amdgcn_sched_barrier(0);
     bool pages_ok = true;
 #pragma unroll
     for (int u = 0; u < PAGES; ++u) pages_ok = pages_ok && ok_page(here.id[u]);
@@ -482,16 +519,21 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a, int
       for (int d = 0; d < NDT; ++d)
 #pragma unroll
         for (int pg = 0; pg < PAGES; ++pg) {
-          const bf16x8 vf = *reinterpret_cast<const bf16x8*>(sm + vad + pg * PGB + d * 1024);
+          const bf16x8 v = *reinterpret_cast<const bf16x8*>(sm + vad + pg * PGB + d * 1024);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) bad |= ((vf[e] & 0x7f80) == 0x7f80 ? 1u : 0u) << (8 * pg + e);
+          for (int e = 0; e < 8; ++e) bad |= ((v[e] & 0x7f80) == 0x7f80 ? 1u : 0u) << (8 * pg + e);
         }
 #pragma unroll
       for (int x = 1; x < 32; x <<= 1) bad |= (unsigned)__shfl_xor((int)bad, x, 64);
     }
-    float mx = sc[0][0];
+    float m4[4], mx;
 #pragma unroll
-    for (int x = 1; x < 32; ++x) mx = __builtin_elementwise_maximum(mx, sc[x >> 4][x & 15]);
+    for (int x = 0; x < 4; ++x) m4[x] = sc[x >> 1][8 * (x & 1)];
+#pragma unroll
+    for (int y = 1; y < 8; ++y)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) m4[x] = __builtin_elementwise_maximum(m4[x], sc[x >> 1][8 * (x & 1) + y]);
+    mx = __builtin_elementwise_maximum(__builtin_elementwise_maximum(m4[0], m4[1]), __builtin_elementwise_maximum(m4[2], m4[3]));
     {
       const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = __builtin_elementwise_maximum(__uint_as_float(h[0]), __uint_as_float(h[1])) * sl2;
@@ -514,29 +556,26 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttnArgs a, int
       lsum = __builtin_amdgcn_fdot2_f32_bf16(pk, one, lsum, false);
       pf[x >> 3][x >> 1 & 3] = __builtin_bit_cast(unsigned, pk);
     }
-    if (!__ballot(bad != 0)) {
+    late_v();
+    const bool any_bad = __ballot(bad != 0) != 0;
+    if (any_bad) {                                      // the product without those keys
 #pragma unroll
-      for (int pg = 0; pg < PAGES; ++pg)
+      for (int pg = 0; pg < PAGES; ++pg) {
+        u32x4 keep;
 #pragma unroll
-        for (int d = 0; d < NDT; ++d) {
-          const bf16x8 vf = *reinterpret_cast<const bf16x8*>(sm + vad + pg * PGB + d * 1024);
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pf[pg]), o[d], 0, 0, 0);
-        }
-      continue;
-    }
+        for (int e = 0; e < 4; ++e)
+          keep[e] = (bad >> (8 * pg + 2 * e) & 1 ? 0u : 0xffffu) | (bad >> (8 * pg + 2 * e + 1) & 1 ? 0u : 0xffff0000u);
 #pragma unroll
-    for (int pg = 0; pg < PAGES; ++pg) {                // the product without those keys
-      u32x4 keep;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        keep[e] = (bad >> (8 * pg + 2 * e) & 1 ? 0u : 0xffffu) | (bad >> (8 * pg + 2 * e + 1) & 1 ? 0u : 0xffff0000u);
-#pragma unroll
-      for (int d = 0; d < NDT; ++d) {
-        const u32x4 vf = *reinterpret_cast<const u32x4*>(sm + vad + pg * PGB + d * 1024) & keep;
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pf[pg]),
-                                                       o[d], 0, 0, 0);
+        for (int d = 0; d < NDT; ++d) vf[pg][d] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, vf[pg][d]) & keep);
       }
     }
+#pragma unroll
+    for (int pg = 0; pg < PAGES; ++pg)
+#pragma unroll
+      for (int d = 0; d < NDT; ++d)
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[pg][d], __builtin_bit_cast(bf16x8, pf[pg]), o[d], 0, 0, 0);
+    next_pages();
+    if (!any_bad) continue;
 #pragma unroll 1
     for (int gg = 0; gg < 2; ++gg) {
 #pragma unroll 1
