@@ -46,11 +46,12 @@ struct PagedAttnArgs {
   int max_rows, max_kv;          // expected longest sequence of rows and of keys (choices only)
   float* part_o; float* part_ml; // split partials, see paged_attn.hip
 };
-// Key splits of a call: z partial results per row (1: none), `shared` of them over the prefix.
+// Key splits of a call.
 struct PagedPlan {
   int splits;                    // of the sequences' own keys
-  int shared;                    // of the shared prefix (0: no prefix pass)
-  int z() const { return splits + shared; }
+  int shared;                    // of the shared prefix (0: no pass of its own)
+  // partial results per row: those of the prefix come first; one split of the rest joins them itself
+  int parts() const { return shared + (splits > 1 ? splits : 0); }
 };
 PagedPlan paged_plan(const PagedAttnArgs& a, int elem_bytes);
 // Floats of part_o and part_ml.

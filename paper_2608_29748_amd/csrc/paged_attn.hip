@@ -9,8 +9,9 @@
 //
 // Visible keys of a row: [lo, hi) and the sinks [0, snk), snk <= lo:
 //   window      hi = p + 1, lo = p - window + 1, snk = sinks
-//   prefix      keys [0, prefix) in one pass over the rows of all sequences, whose tiles so
-//               fill with rows that read the same pages; [prefix, p] sequence by sequence.
+//   prefix      where it pays, keys [0, prefix) in a pass over the rows of all sequences, whose
+//               tiles so fill with rows that read the same pages, and then [prefix, p] sequence
+//               by sequence, joined with what the first pass left.
 #include "paged.h"
 
 namespace rt {
@@ -18,14 +19,25 @@ namespace rt {
 typedef __attribute__((address_space(4))) const int32_t const_i32_t;
 
 constexpr int kStep = 32;                  // keys per step of a wave: two pages
+constexpr int kMaxParts = 32;              // key splits of a pass
 constexpr float kMrefInit = -1.0e30f;      // running maximum before any visible key (log2 units)
 
+// One launch of a call: over the shared prefix, or over the sequences' own keys (all of them where
+// no pass is made over the prefix).
+struct PagedPass {
+  int shared;       // 1: the rows of all sequences over the prefix
+  int first;        // key from which on the sequences' own pass works (0, or the prefix)
+  int splits;
+  int z0;           // partial results go to parts z0 .. z0 + splits - 1; -1: rows are finished here,
+  int join;         // together with parts 0 .. join - 1
+};
+
 struct RowRange { int lo, hi, snk; };
-__device__ __forceinline__ RowRange row_range(const PagedAttnArgs& a, bool shared, long pos, int keys) {
+__device__ __forceinline__ RowRange row_range(const PagedAttnArgs& a, const PagedPass& ps, long pos, int keys) {
   const long cap = (long)a.r.max_pages * kPage;
   long hi = a.causal ? pos + 1 : (long)keys;
-  hi = max(0l, min(hi, shared ? min(cap, (long)a.prefix) : cap));
-  long lo = shared ? 0 : (long)a.prefix;
+  hi = max(0l, min(hi, ps.shared ? min(cap, (long)a.prefix) : cap));
+  long lo = ps.first;
   if (a.window > 0) lo = max(lo, pos - a.window + 1);
   lo = min(max(lo, 0l), hi);
   return RowRange{(int)lo, (int)hi, (int)min((long)a.sinks, lo)};
@@ -45,10 +57,10 @@ struct Steps {
 };
 
 // What the row (of the call) tok sees; sr: its sequence, where the block has one.
-__device__ __forceinline__ RowRange lane_range(const PagedAttnArgs& a, bool shared, const SeqRows& sr, int tok) {
+__device__ __forceinline__ RowRange lane_range(const PagedAttnArgs& a, const PagedPass& ps, const SeqRows& sr, int tok) {
   const PagedRows& r = a.r;
   SeqRows q = sr;
-  if (shared) {
+  if (ps.shared) {
     int sq = tok;
     if (r.row_start) {            // the last sequence that starts at or before the row
       int b = 0, e = r.n_seqs;
@@ -63,7 +75,7 @@ __device__ __forceinline__ RowRange lane_range(const PagedAttnArgs& a, bool shar
     q = seq_rows(r, sq);
     if (tok < q.a || tok >= q.a + q.n) return RowRange{0, 0, 0};     // a row of no sequence
   }
-  return row_range(a, shared, (long)q.keys - q.n + (tok - q.a), q.keys);
+  return row_range(a, ps, (long)q.keys - q.n + (tok - q.a), q.keys);
 }
 // Sequence and row block of block blk, of `per` (token, head) rows each; false: none.  The results
 // are the same for every lane and made scalar, so that page ids come by scalar loads.
@@ -90,31 +102,38 @@ __device__ __forceinline__ bool block_rows(const PagedAttnArgs& a, bool shared, 
   return true;
 }
 
-// Page table row of sequence s (the same for every lane), as a pointer for scalar loads.
-__device__ __forceinline__ const_i32_t* table_row(const PagedRows& r, int s) {
-  const uint64_t p = (uint64_t)(r.page_table + (size_t)s * r.max_pages);
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)p), hi = __builtin_amdgcn_readfirstlane((uint32_t)(p >> 32));
-  return (const_i32_t*)((uint64_t)hi << 32 | lo);
-}
-// Over all lanes, in a scalar register.
-__device__ __forceinline__ int wave_min(int v) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) v = min(v, __shfl_xor(v, o, 64));
-  return __builtin_amdgcn_readfirstlane(v);
-}
-__device__ __forceinline__ int wave_max(int v) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) v = max(v, __shfl_xor(v, o, 64));
-  return __builtin_amdgcn_readfirstlane(v);
-}
+// The pages of sequence s (the same for every lane; scalar loads for scalar indexes): those of the
+// shared prefix through the first sequence's row of the table.
+struct TableRow {
+  const_i32_t* own;
+  const_i32_t* first;
+  int n_first;
+  __device__ __forceinline__ TableRow(const PagedAttnArgs& a, int s) {
+    const uint64_t p = (uint64_t)(a.r.page_table + (size_t)s * a.r.max_pages);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)p), hi = __builtin_amdgcn_readfirstlane((uint32_t)(p >> 32));
+    own = (const_i32_t*)((uint64_t)hi << 32 | lo);
+    first = (const_i32_t*)a.r.page_table;
+    n_first = a.prefix / kPage;
+  }
+  __device__ __forceinline__ int page(int j) const { return (j < n_first ? first : own)[j]; }
+};
+// wave-wide integer reductions of the ROCm device library (DPP based), in a scalar register
+extern "C" __device__ int __ockl_wfred_min_i32(int);
+extern "C" __device__ int __ockl_wfred_max_i32(int);
+__device__ __forceinline__ int wave_min(int v) { return __builtin_amdgcn_readfirstlane(__ockl_wfred_min_i32(v)); }
+__device__ __forceinline__ int wave_max(int v) { return __builtin_amdgcn_readfirstlane(__ockl_wfred_max_i32(v)); }
 
 // Rows kernel: one workgroup of NW waves per block of 16 NT (token, head) rows, KV head and key
 // split.  Every wave takes every NW-th step of 32 keys of the split straight from memory into
 // registers in MFMA operand order (S^T = K Q^T, O^T = V^T P^T; the K rows of a 16-row tile are
 // the keys 8(r/4) + 4 tile + r%4, so that a lane ends up with eight consecutive keys of its
-// query, whose V^T fragment is one contiguous read); the waves' results meet in LDS.
-template <typename T, int HD, int NT, int NW>
-__global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, int shared, int splits, int z0, int zs) {
+// query, whose V^T fragment is one contiguous read); the waves' results meet in LDS.  Bound by
+// memory: two waves per SIMD with one step of 16 KB (bf16, head_dim 128) each under way, and pages
+// that only this workgroup reads come by non-temporal loads (NTL).  64 steps over 4100 keys, 40 heads
+// (1.08 GB): 165 us (6.5 TB/s); with plain loads 185, with three waves per SIMD 197, with a second set
+// of registers for the next step's keys 208.
+template <typename T, int HD, int NT, int NW, bool NTL>
+__global__ __launch_bounds__(64 * NW, 2) void paged_rows_kernel(PagedAttnArgs a, PagedPass ps) {
   constexpr int NHT = HD / 16, NKS = HD / 32;
   constexpr int RB = 16 * NT;
   constexpr int OP = HD + 4;                               // fp32 pitch of a merged row
@@ -124,12 +143,12 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, in
   const PagedRows& r = a.r;
   const int lane = threadIdx.x & 63, g4 = lane >> 4, c16 = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = blockIdx.x % r.n_kv_heads, split = blockIdx.x / r.n_kv_heads % splits;
-  const int blk = blockIdx.x / (r.n_kv_heads * splits);
+  const int kvh = blockIdx.x % r.n_kv_heads, split = blockIdx.x / r.n_kv_heads % ps.splits;
+  const int blk = blockIdx.x / (r.n_kv_heads * ps.splits);
   const int G = r.n_q_heads / r.n_kv_heads;
   int s, rb;
   SeqRows sr;
-  if (!block_rows(a, shared, blk, RB, s, rb, sr)) return;
+  if (!block_rows(a, ps.shared, blk, RB, s, rb, sr)) return;
   const int nrows = sr.n * G, row0 = rb * RB;
   if (row0 >= nrows) return;
 
@@ -141,7 +160,7 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, in
   for (int t = 0; t < NT; ++t) {
     const int rr = min(row0 + t * 16 + c16, nrows - 1);
     const int tok = sr.a + rr / G;
-    rg[t] = lane_range(a, shared, sr, tok);
+    rg[t] = lane_range(a, ps, sr, tok);
     const T* qp = (const T*)a.q + (size_t)tok * a.ldq + (size_t)(kvh * G + rr % G) * HD;
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks) qf[t][ks].load(qp + ks * 32 + g4 * 8);
@@ -159,10 +178,11 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, in
   all_snk = wave_max(all_snk);
   min_snk = wave_min(min_snk);
   const Steps<kStep> st(all_snk, all_lo, all_hi);
-  const int per = (st.n + splits - 1) / splits;
-  const int i_end = min(st.n, (split + 1) * per);
+  const int per = (st.n + ps.splits - 1) / ps.splits;
+  const int i_beg = split * per + w, i_end = min(st.n, (split + 1) * per);
+  const int n = i_end > i_beg ? (i_end - i_beg + NW - 1) / NW : 0;      // this wave's steps
 
-  const_i32_t* pt = table_row(r, s);
+  const TableRow pt(a, s);
   const int last_page = max(0, (all_hi - 1) / kPage);
   const float sl2 = a.scale * 1.4426950408889634f;
   float mref[NT], lsum[NT];
@@ -175,23 +195,42 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, in
     for (int h = 0; h < NHT; ++h) o[t][h] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  for (int i = split * per + w; i < i_end; i += NW) {
-    const int k0 = st.key(i);
-    const int p0 = pt[min(k0 / kPage, last_page)], p1 = pt[min(k0 / kPage + 1, last_page)];
-    const bool ok0 = p0 >= 0 && p0 < r.n_pages, ok1 = p1 >= 0 && p1 < r.n_pages;
-    const size_t PE = (size_t)kPage * HD;
-    const size_t b0 = ((size_t)(ok0 ? p0 : 0) * r.n_kv_heads + kvh) * PE;
-    const size_t b1 = ((size_t)(ok1 ? p1 : 0) * r.n_kv_heads + kvh) * PE;
-    const T* kp = (const T*)r.k + ((c16 >> 3) ? b1 : b0) + (size_t)(8 * ((c16 >> 2) & 1) + (c16 & 3)) * HD + g4 * 8;
-    const T* vp = (const T*)r.v + ((g4 >> 1) ? b1 : b0) + (size_t)c16 * kPage + (g4 & 1) * 8;
-    Frag<T> kf[2][NKS], vf[NHT];
+  const size_t PE = (size_t)kPage * HD;
+  const int ko = (8 * ((c16 >> 2) & 1) + (c16 & 3)) * HD + g4 * 8, vo = c16 * kPage + (g4 & 1) * 8;
+  struct Keys {
+    Frag<T> k[2][NKS], v[NHT];
+    size_t b0, b1;                      // the two pages
+    int k0;
+    bool ok0, ok1;
+  };
+  // page ids of 32 steps at a time, a lane each
+  int ids = 0;
+  auto fetch = [&](Keys& f, int t) {    // this wave's step t
+    if ((t & 31) == 0) ids = pt.page(min(st.key(i_beg + min(t + (lane >> 1), n - 1) * NW) / kPage + (lane & 1), last_page));
+    const int p0 = __builtin_amdgcn_readlane(ids, 2 * (t & 31)), p1 = __builtin_amdgcn_readlane(ids, 2 * (t & 31) + 1);
+    f.k0 = st.key(i_beg + t * NW);
+    f.ok0 = p0 >= 0 && p0 < r.n_pages;
+    f.ok1 = p1 >= 0 && p1 < r.n_pages;
+    f.b0 = ((size_t)(f.ok0 ? p0 : 0) * r.n_kv_heads + kvh) * PE;
+    f.b1 = ((size_t)(f.ok1 ? p1 : 0) * r.n_kv_heads + kvh) * PE;
+    const T* kp = (const T*)r.k + ((c16 >> 3) ? f.b1 : f.b0) + ko;
+    const T* vp = (const T*)r.v + ((g4 >> 1) ? f.b1 : f.b0) + vo;
 #pragma unroll
     for (int ta = 0; ta < 2; ++ta)
 #pragma unroll
-      for (int ks = 0; ks < NKS; ++ks) kf[ta][ks].load(kp + ta * 4 * HD + ks * 32);
+      for (int ks = 0; ks < NKS; ++ks) {
+        if constexpr (NTL) f.k[ta][ks].load_stream(kp + ta * 4 * HD + ks * 32);
+        else f.k[ta][ks].load(kp + ta * 4 * HD + ks * 32);
+      }
 #pragma unroll
-    for (int h = 0; h < NHT; ++h) vf[h].load(vp + h * 16 * kPage);
-    const bool whole = ok0 && ok1 && k0 + kStep <= min_hi && (k0 >= max_lo || k0 + kStep <= min_snk);
+    for (int h = 0; h < NHT; ++h) {
+      if constexpr (NTL) f.v[h].load_stream(vp + h * 16 * kPage);
+      else f.v[h].load(vp + h * 16 * kPage);
+    }
+  };
+  auto use = [&](Keys& f) {
+    const int k0 = f.k0;
+    const bool whole = f.ok0 && f.ok1 && k0 + kStep <= min_hi && (k0 >= max_lo || k0 + kStep <= min_snk);
     // keys (of the 32) with a non-finite V element somewhere: a weight of zero must not meet
     // them in a product, so where rows differ in what they see they are added one by one
     uint32_t bad = 0;
@@ -200,7 +239,7 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, in
 #pragma unroll
       for (int h = 0; h < NHT; ++h)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) mine |= (__builtin_isfinite(vf[h].get(e)) ? 0u : 1u) << e;
+        for (int e = 0; e < 8; ++e) mine |= (__builtin_isfinite(f.v[h].get(e)) ? 0u : 1u) << e;
 #pragma unroll
       for (int x = 1; x < 16; x <<= 1) mine |= __shfl_xor((int)mine, x, 64);
       if (__ballot(mine != 0)) {
@@ -208,7 +247,7 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, in
         for (int e = 0; e < 8; ++e)
           if (mine >> e & 1)
 #pragma unroll
-            for (int h = 0; h < NHT; ++h) vf[h].set(e, 0.f);
+            for (int h = 0; h < NHT; ++h) f.v[h].set(e, 0.f);
 #pragma unroll
         for (int x = 0; x < 4; ++x) bad |= (uint32_t)__builtin_amdgcn_readlane((int)mine, 16 * x) << (8 * x);
       }
@@ -219,11 +258,11 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, in
       sc[0] = sc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < NKS; ++ks) {
-        mma(sc[0], kf[0][ks], qf[t][ks]);
-        mma(sc[1], kf[1][ks], qf[t][ks]);
+        mma(sc[0], f.k[0][ks], qf[t][ks]);
+        mma(sc[1], f.k[1][ks], qf[t][ks]);
       }
       if (!whole) {
-        const bool ok = g4 < 2 ? ok0 : ok1;
+        const bool ok = g4 < 2 ? f.ok0 : f.ok1;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int j = k0 + 8 * g4 + e;
@@ -261,8 +300,8 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, in
       }
 #pragma unroll
       for (int h = 0; h < NHT; ++h) {
-        mma(o[t][h], vf[h], ph);
-        if constexpr (sizeof(T) == 2) mma(o[t][h], vf[h], pl);
+        mma(o[t][h], f.v[h], ph);
+        if constexpr (sizeof(T) == 2) mma(o[t][h], f.v[h], pl);
       }
       if (bad) {
 #pragma unroll
@@ -271,7 +310,7 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, in
         for (uint32_t m = bad; m; m &= m - 1) {
           const int j = __builtin_ctz(m);
           const float pj = *(volatile float*)&sP[w][j][c16];
-          const T* vj = (const T*)r.v + (j < 16 ? b0 : b1) + (j & 15) + (size_t)(4 * g4) * kPage;
+          const T* vj = (const T*)r.v + (j < 16 ? f.b0 : f.b1) + (j & 15) + (size_t)(4 * g4) * kPage;
 #pragma unroll
           for (int h = 0; h < NHT; ++h)
 #pragma unroll
@@ -280,8 +319,15 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, in
         }
       }
     }
+  };
+  for (int t = 0; t < n; ++t) {
+    Keys f;
+    fetch(f, t);
+    use(f);
   }
-  // join the waves
+  // join the waves: thread i takes eight elements of a row
+  constexpr int RUNS = HD / 8;
+  static_assert(RB * RUNS <= 64 * NW, "a thread per item");
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const float l = group4_sum(lsum[t]);
@@ -294,45 +340,84 @@ __global__ __launch_bounds__(64 * NW) void paged_rows_kernel(PagedAttnArgs a, in
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < RB * (HD / 8); i += 64 * NW) {
-    const int rl = i / (HD / 8), d = i % (HD / 8) * 8, rr = row0 + rl;
-    if (rr >= nrows) continue;
-    const int tok = sr.a + rr / G, h = kvh * G + rr % G;
-    float M = sML[0][rl][0];
+  const int items = min(RB, nrows - row0) * RUNS;
+  const size_t zst = (size_t)r.n_rows * r.n_q_heads;
+  const int it = threadIdx.x % items, grp = threadIdx.x / items;      // (groups: the prefix parts, below)
+  const int rl = it / RUNS, d = it % RUNS * 8, rr = row0 + rl;
+  const int tok = sr.a + rr / G, h = kvh * G + rr % G;
+  const size_t rh = (size_t)tok * r.n_q_heads + h;
+  float M = sML[0][rl][0], L = 0.f, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int u = 1; u < NW; ++u) M = fmaxf(M, sML[u][rl][0]);
-    float L = 0.f, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int u = 1; u < NW; ++u) M = fmaxf(M, sML[u][rl][0]);
 #pragma unroll
-    for (int u = 0; u < NW; ++u) {
-      const float f = __builtin_amdgcn_exp2f(sML[u][rl][0] - M);
-      L += f * sML[u][rl][1];
+  for (int u = 0; u < NW; ++u) {
+    const float f = __builtin_amdgcn_exp2f(sML[u][rl][0] - M);
+    L += f * sML[u][rl][1];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += f * sO[u][rl][d + e];
+    for (int e = 0; e < 8; ++e) v[e] += f * sO[u][rl][d + e];
+  }
+  if (ps.join) {
+    // with the prefix: its parts' maxima and sums through LDS, its elements shared out over as many
+    // threads per item as there are
+    const int zs = ps.join, groups = 64 * NW / items;
+    float2* const pml = reinterpret_cast<float2*>(&sP[0][0][0]);
+    static_assert(sizeof(sP) >= RB * kMaxParts * sizeof(float2), "maxima and sums of the parts");
+    for (int i = threadIdx.x; i < items / RUNS * zs; i += 64 * NW) {
+      const int row = row0 + i / zs, tk = sr.a + row / G, hd = kvh * G + row % G;
+      pml[i] = *reinterpret_cast<const float2*>(a.part_ml + ((i % zs) * zst + (size_t)tk * r.n_q_heads + hd) * 2);
     }
-    if (zs > 1) {
-      const size_t row = ((size_t)(z0 + split) * r.n_rows + tok) * r.n_q_heads + h;
-      float* op = a.part_o + row * HD + d;
-      *reinterpret_cast<float4*>(op) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(op + 4) = make_float4(v[4], v[5], v[6], v[7]);
-      if (d == 0) {
-        a.part_ml[row * 2] = M;
-        a.part_ml[row * 2 + 1] = L;
-      }
-    } else {
-      const float inv = L == 0.f ? 0.f : 1.f / L;       // (NaN stays NaN)
-      Frag<T> f;
+    __syncthreads();
+    float m = M;
+    for (int z = 0; z < zs; ++z) m = fmaxf(m, pml[rl * zs + z].x);
+    const float f0 = __builtin_amdgcn_exp2f(M - m);
+    L *= f0;
+    for (int z = 0; z < zs; ++z) L += __builtin_amdgcn_exp2f(pml[rl * zs + z].x - m) * pml[rl * zs + z].y;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f.set(e, L == 0.f ? 0.f : v[e] * inv);
-      const size_t at = a.packed ? pa_index(tok, h * HD + d, (size_t)a.ldo) : (size_t)tok * a.ldo + (size_t)h * HD + d;
-      f.store((T*)a.out + at);
+    for (int e = 0; e < 8; ++e) v[e] = grp == 0 ? v[e] * f0 : 0.f;
+    if (grp < groups) {
+      const float* op = a.part_o + rh * HD + d;
+#pragma unroll 4
+      for (int z = grp; z < zs; z += groups) {
+        const float f = __builtin_amdgcn_exp2f(pml[rl * zs + z].x - m);
+        const float4 a0 = *reinterpret_cast<const float4*>(op + z * zst * HD);
+        const float4 a1 = *reinterpret_cast<const float4*>(op + z * zst * HD + 4);
+        v[0] += f * a0.x; v[1] += f * a0.y; v[2] += f * a0.z; v[3] += f * a0.w;
+        v[4] += f * a1.x; v[5] += f * a1.y; v[6] += f * a1.z; v[7] += f * a1.w;
+      }
+    }
+    if (groups > 1) {
+      float* const sv = &sO[0][0][0];                  // [group][item][8] (every wave is past its reads)
+      if (grp > 0 && grp < groups)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sv[(grp * items + it) * 8 + e] = v[e];
+      __syncthreads();
+      if (grp == 0)
+        for (int u = 1; u < groups; ++u)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] += sv[(u * items + it) * 8 + e];
     }
   }
+  if (grp > 0) return;
+  if (ps.z0 >= 0) {
+    const size_t row = (ps.z0 + split) * zst + rh;
+    float* op = a.part_o + row * HD + d;
+    *reinterpret_cast<float4*>(op) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(op + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    *reinterpret_cast<float2*>(a.part_ml + row * 2) = make_float2(M, L);      // (the same from every lane of the row)
+    return;
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;       // (NaN stays NaN)
+  Frag<T> f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f.set(e, L == 0.f ? 0.f : v[e] * inv);
+  const size_t at = a.packed ? pa_index(tok, h * HD + d, (size_t)a.ldo) : (size_t)tok * a.ldo + (size_t)h * HD + d;
+  f.store((T*)a.out + at);
 }
 
 // Tile kernel (bf16, many rows per page): one workgroup of four waves per block of 128 (token,
 // head) rows, KV head and key split.  A wave owns 32 rows, one per column of 32x32x16 MFMAs; chunks of
 // 64 keys (four pages of K, four of V, one of each copied by every wave straight into LDS) pass
-// through two LDS stages, the copies of the next chunk in flight while one is used, one barrier a
+// through NST LDS stages, the copies of the next chunks in flight while one is used, one barrier a
 // chunk.  S^T = K Q^T with the K rows of a page taken in the order that swaps bits 2 and 3 of the
 // row, so that a lane's eight scores of a page belong to eight consecutive keys, which is the
 // B operand of O^T = V^T P^T as it stands, and V^T's fragments are contiguous 1 KiB reads.  K rows
@@ -350,58 +435,44 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 // the 16 bytes at off[j] + j * step of every lane to dst + 1024 j + 16 lane.  Buffer copies: after a
 // global one, which counts as flat, every wait for LDS reads would be a full one.
 template <int N>
-__device__ __forceinline__ void copy_page(const char* src, char* dst, const int (&off)[N], int step) {
+__device__ __forceinline__ void copy_page(const char* src, char* dst, const int* off, int step) {
   const __amdgpu_buffer_rsrc_t b = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), 0, N * 1024, 0x00027000);
 #pragma unroll
   for (int j = 0; j < N; ++j)
     __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (lds_void_t*)(dst + j * 1024), 16, off[j], j * step, 0, 0);
 }
 
-template <int HD>
-__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void paged_tile_kernel(PagedAttnArgs a, int shared, int splits, int z0, int zs) {
+template <int HD, int NST>
+__global__ __launch_bounds__(256, NST > 2 ? 1 : HD == 64 ? 3 : 2) void paged_tile_kernel(PagedAttnArgs a, PagedPass ps) {
   constexpr int ROWB = HD * 2, NP = ROWB / 16, PGB = kPage * ROWB, NLD = PGB / 1024;
   constexpr int PAGES = kChunkT / kPage, STG = 2 * PAGES * PGB;
   constexpr int NKS = HD / 16, NDT = HD / 32;
   constexpr int OPB = ROWB + 16;                       // pitch of a finished row in LDS
   static_assert(2 * STG >= kTileRows * OPB, "finished rows fit the stages");
-  __shared__ __attribute__((aligned(1024))) char smem[2 * STG];
+  static_assert(NST == 2 || NST == 4, "stage offsets wrap by a mask");
+  __shared__ __attribute__((aligned(1024))) char smem[NST * STG];
   const PagedRows& r = a.r;
   const int lane = threadIdx.x & 63, g = lane >> 5, c32 = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = blockIdx.x % r.n_kv_heads, split = blockIdx.x / r.n_kv_heads % splits;
-  const int blk = blockIdx.x / (r.n_kv_heads * splits);
+  const int kvh = blockIdx.x % r.n_kv_heads, split = blockIdx.x / r.n_kv_heads % ps.splits;
+  const int blk = blockIdx.x / (r.n_kv_heads * ps.splits);
   const int G = r.n_q_heads / r.n_kv_heads;
   int s, rb;
   SeqRows sr;
-  if (!block_rows(a, shared, blk, kTileRows, s, rb, sr)) return;
+  if (!block_rows(a, ps.shared, blk, kTileRows, s, rb, sr)) return;
   const int nrows = sr.n * G, row0 = rb * kTileRows;
   if (row0 >= nrows) return;
 
   // the keys that any row of the block sees: its first and last rows span them, except over the
   // rows of several sequences, whose prefix passes take all of the prefix
   const int first_tok = sr.a + row0 / G, last_tok = sr.a + (min(nrows, row0 + kTileRows) - 1) / G;
-  const RowRange rf = shared ? RowRange{0, min(a.prefix, r.max_pages * kPage), 0} : lane_range(a, false, sr, first_tok);
-  const RowRange rl = shared ? rf : lane_range(a, false, sr, last_tok);
+  const RowRange rf = ps.shared ? RowRange{0, min(a.prefix, r.max_pages * kPage), 0} : lane_range(a, ps, sr, first_tok);
+  const RowRange rl = ps.shared ? rf : lane_range(a, ps, sr, last_tok);
   const int all_hi = __builtin_amdgcn_readfirstlane(max(rf.hi, rl.hi));
   const Steps<kChunkT> st(__builtin_amdgcn_readfirstlane(max(rf.snk, rl.snk)),
                           __builtin_amdgcn_readfirstlane(min(rf.lo, rl.lo)), all_hi);
-  const int per = (st.n + splits - 1) / splits;
+  const int per = (st.n + ps.splits - 1) / ps.splits;
   const int i_beg = split * per, i_end = min(st.n, i_beg + per);
-
-  // this lane's row
-  const int wrow = row0 + w * 32;
-  const bool live = wrow < nrows;                       // this wave has rows
-  const int rr = min(wrow + c32, nrows - 1);
-  const int tok = sr.a + rr / G, head = kvh * G + rr % G;
-  const RowRange rg = lane_range(a, shared, sr, tok);
-  const int min_hi = wave_min(rg.hi), max_lo = wave_max(rg.lo), min_snk = wave_min(rg.snk);
-  const int max_hi = wave_max(rg.hi), min_lo = wave_min(rg.lo), max_snk = wave_max(rg.snk);
-  Frag<bf16_t> qf[NKS];
-  {
-    const bf16_t* qp = (const bf16_t*)a.q + (size_t)tok * a.ldq + (size_t)head * HD + g * 8;
-#pragma unroll
-    for (int ks = 0; ks < NKS; ++ks) qf[ks].load(qp + ks * 16);
-  }
 
   // source offsets of this wave's copies (LDS slot j * 64 + lane of its page)
   auto swz = [](int row) { return NP == 16 ? row : row >> 1; };
@@ -412,15 +483,15 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void paged_tile_kernel(Paged
     koff[j] = row * ROWB + (pc ^ swz(row)) * 16;
     voff[j] = lane * 16;
   }
-  const_i32_t* pt = table_row(r, s);
+  const TableRow pt(a, s);
   const int last_page = max(0, (all_hi - 1) / kPage);
   struct Pages { int id[PAGES], own; };              // own: the page that this wave copies
   auto pages_at = [&](int i) {
     Pages p;
     const int pg = st.key(i) / kPage;
 #pragma unroll
-    for (int u = 0; u < PAGES; ++u) p.id[u] = pt[min(pg + u, last_page)];
-    p.own = pt[min(pg + w, last_page)];
+    for (int u = 0; u < PAGES; ++u) p.id[u] = pt.page(min(pg + u, last_page));
+    p.own = pt.page(min(pg + w, last_page));
     return p;
   };
   auto ok_page = [&](int id) { return id >= 0 && id < r.n_pages; };
@@ -430,6 +501,33 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void paged_tile_kernel(Paged
     copy_page<NLD>((const char*)r.k + at, l, koff, 0);
     copy_page<NLD>((const char*)r.v + at, l + PAGES * PGB, voff, 1024);
   };
+  // page ids of the chunk in use and of the next NST: the last are asked for at the end of a step
+  // (a scalar load under way would make every LDS wait a full one)
+  Pages ids[NST + 1];
+#pragma unroll
+  for (int x = 0; x <= NST; ++x) ids[x] = Pages{};
+  if (i_beg < i_end) {
+#pragma unroll
+    for (int x = 0; x <= NST; ++x) ids[x] = pages_at(min(i_beg + x, i_end - 1));
+#pragma unroll
+    for (int x = 0; x < NST - 1; ++x)
+      if (i_beg + x < i_end) issue(ids[x], x * STG);
+  }
+  // this lane's row
+  const int wrow = row0 + w * 32;
+  const bool live = wrow < nrows;                       // this wave has rows
+  const int rr = min(wrow + c32, nrows - 1);
+  const int tok = sr.a + rr / G, head = kvh * G + rr % G;
+  const RowRange rg = lane_range(a, ps, sr, tok);
+  const int min_hi = wave_min(rg.hi), max_lo = wave_max(rg.lo), min_snk = wave_min(rg.snk);
+  const int max_hi = wave_max(rg.hi), min_lo = wave_min(rg.lo), max_snk = wave_max(rg.snk);
+  Frag<bf16_t> qf[NKS];
+  {
+    const bf16_t* qp = (const bf16_t*)a.q + (size_t)tok * a.ldq + (size_t)head * HD + g * 8;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) qf[ks].load(qp + ks * 16);
+  }
+
   // read offsets: K fragment ks of the tile's rows, V fragments
   const int krow = (c32 & 16) * 1 + ((c32 & 4) << 1) + ((c32 & 8) >> 1) + (c32 & 3);   // bits 2 and 3 swapped
   // (piece 2 ks + g of the row, permuted: the pieces of ks differ from those of 0 in bits alone)
@@ -444,27 +542,21 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void paged_tile_kernel(Paged
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
 
-  // page ids of the chunk in use and of the next two: the last are asked for at the end of a
-  // step (a scalar load under way would make every LDS wait a full one)
-  Pages cur{}, nxt{}, far{};
-  if (i_beg < i_end) {
-    cur = pages_at(i_beg);
-    issue(cur, 0);
-    nxt = pages_at(min(i_beg + 1, i_end - 1));
-    far = pages_at(min(i_beg + 2, i_end - 1));
-  }
   int stage = 0;
   for (int i = i_beg; i < i_end; ++i) {
-    wait_vm<0>();      // this wave's copies of chunk i have landed
+    // this wave's copies of chunk i have landed, those of later ones may be under way
+    if (NST == 4 && i + 2 < i_end) wait_vm<(NST - 2) * 2 * NLD>();
+    else if (NST == 4 && i + 1 < i_end) wait_vm<2 * NLD>();
+    else wait_vm<0>();
     lds_barrier();     // everyone's have; chunk i-1's stage is free
-    const Pages here = cur;
-    if (i + 1 < i_end) issue(nxt, stage ^ STG);
-    cur = nxt;
-    nxt = far;
-    auto next_pages = [&]() { far = pages_at(min(i + 3, i_end - 1)); };
+    const Pages here = ids[0];
+    if (i + NST - 1 < i_end) issue(ids[NST - 1], (stage + (NST - 1) * STG) & (NST * STG - 1));
+#pragma unroll
+    for (int x = 0; x < NST; ++x) ids[x] = ids[x + 1];
+    auto next_pages = [&]() { ids[NST] = pages_at(min(i + NST + 1, i_end - 1)); };
     const int k0 = st.key(i);
     const char* sm = smem + stage;
-    stage ^= STG;
+    stage = (stage + STG) & (NST * STG - 1);
     // (a wave none of whose rows sees the chunk passes it by)
     if (!live || !((k0 < max_hi && k0 + kChunkT > min_lo) || k0 < max_snk)) {
       next_pages();
@@ -602,9 +694,10 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void paged_tile_kernel(Paged
     lsum = __uint_as_float(h[0]) + __uint_as_float(h[1]);
   }
   const bool row_ok = wrow + c32 < nrows;
-  if (zs > 1) {
+  const size_t rh = (size_t)tok * r.n_q_heads + head, zst = (size_t)r.n_rows * r.n_q_heads;
+  if (ps.z0 >= 0) {
     if (!row_ok) return;
-    const size_t row = ((size_t)(z0 + split) * r.n_rows + tok) * r.n_q_heads + head;
+    const size_t row = (ps.z0 + split) * zst + rh;
     float* op = a.part_o + row * HD;
 #pragma unroll
     for (int d = 0; d < NDT; ++d)
@@ -617,6 +710,30 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void paged_tile_kernel(Paged
       a.part_ml[row * 2 + 1] = lsum;
     }
     return;
+  }
+  if (ps.join) {       // with the parts of the prefix
+#pragma unroll 2
+    for (int z = 0; z < ps.join; ++z) {
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (z * zst + rh) * 2);
+      const float* op = a.part_o + (z * zst + rh) * HD + 4 * g;
+      float4 p[NDT][4];
+#pragma unroll
+      for (int d = 0; d < NDT; ++d)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) p[d][b] = *reinterpret_cast<const float4*>(op + d * 32 + 8 * b);
+      const float M = fmaxf(mref, ml.x), f0 = __builtin_amdgcn_exp2f(mref - M), f = __builtin_amdgcn_exp2f(ml.x - M);
+      mref = M;
+      lsum = f0 * lsum + f * ml.y;
+#pragma unroll
+      for (int d = 0; d < NDT; ++d)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          o[d][4 * b] = f0 * o[d][4 * b] + f * p[d][b].x;
+          o[d][4 * b + 1] = f0 * o[d][4 * b + 1] + f * p[d][b].y;
+          o[d][4 * b + 2] = f0 * o[d][4 * b + 2] + f * p[d][b].z;
+          o[d][4 * b + 3] = f0 * o[d][4 * b + 3] + f * p[d][b].w;
+        }
+    }
   }
   // finished rows through LDS, so that they leave 16 bytes a lane along the row
   const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
@@ -686,9 +803,6 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a, int z
 }
 
 // ------------------------------------------------------------------ host
-constexpr int kRowsNT = 1;
-constexpr int kRowsNW = 4;
-
 static long row_blocks(const PagedAttnArgs& a, bool shared, int rb) {
   const PagedRows& r = a.r;
   const int G = r.n_q_heads / r.n_kv_heads;
@@ -696,32 +810,57 @@ static long row_blocks(const PagedAttnArgs& a, bool shared, int rb) {
   if (r.row_start) return (long)r.n_rows * G / rb + r.n_seqs;
   return (long)r.n_seqs * (((long)r.rows_each * G + rb - 1) / rb);
 }
-// bf16 blocks of more than 16 (token, head) rows take the tile kernel.
+// Rows of a sequence (of all of them, over the prefix) for a KV head, as far as the host knows.
+static long rows_of(const PagedAttnArgs& a, bool shared) {
+  return (long)(shared ? a.r.n_rows : a.max_rows) * (a.r.n_q_heads / a.r.n_kv_heads);
+}
+// Query tiles of a wave of the rows kernel: two where fp32 rows fill them and the registers hold them,
+// so that a page is read half as often.
+static int rows_nt(const PagedAttnArgs& a, bool shared, int elem_bytes) {
+  return elem_bytes == 4 && a.r.head_dim == 64 && rows_of(a, shared) > 16 ? 2 : 1;
+}
+// bf16 passes of more than 16 (token, head) rows a block take the tile kernel.
 static bool tiled(const PagedAttnArgs& a, bool shared, int elem_bytes) {
+  return elem_bytes == 2 && rows_of(a, shared) > 16;
+}
+static int block_size(const PagedAttnArgs& a, bool shared, int elem_bytes) {
+  return tiled(a, shared, elem_bytes) ? kTileRows : 16 * rows_nt(a, shared, elem_bytes);
+}
+
+// Keys of a sequence that a pass from key `first` on reads, as far as the host knows.
+static long keys_of(const PagedAttnArgs& a, long first) {
+  const long keys = a.max_kv - first, seen = (long)a.window + a.sinks + a.max_rows;
+  return a.window > 0 && keys > seen ? seen : keys < 0 ? 0 : keys;
+}
+// Whether the rows kernel's pages come by non-temporal loads: where each is read by one workgroup
+// and all of them are more than the 256 MB memory-side cache holds (1.08 GB: 165 us against 185;
+// 134 MB that lay in that cache: 41 us against 30).
+static bool streamed(const PagedAttnArgs& a, long first, int elem_bytes) {
   const PagedRows& r = a.r;
-  return elem_bytes == 2 && (long)(shared ? r.n_rows : a.max_rows) * (r.n_q_heads / r.n_kv_heads) > 16 * kRowsNT;
+  return a.prefix <= first && 2.0 * r.n_seqs * keys_of(a, first) * r.n_kv_heads * r.head_dim * elem_bytes > 256e6;
 }
 
 PagedPlan paged_plan(const PagedAttnArgs& a, int elem_bytes) {
   const PagedRows& r = a.r;
   PagedPlan p{1, 0};
+  // A pass over the shared prefix of its own pays where the sequences' rows do not fill tiles by
+  // themselves and reading the prefix once for each would move much more than reading it once.
+  const double pre = 2.0 * a.prefix * r.n_kv_heads * r.head_dim * elem_bytes;
+  const bool apart = a.prefix > 0 && rows_of(a, false) < kTileRows && (r.n_seqs - 1.33) * pre > 40e6;
   auto pick = [&](bool shared, long keys) {
-    const bool t = tiled(a, shared, elem_bytes);
-    const long units = row_blocks(a, shared, t ? kTileRows : 16 * kRowsNT) * r.n_kv_heads;
+    const long units = row_blocks(a, shared, block_size(a, shared, elem_bytes)) * r.n_kv_heads;
     long s = 512 / units;
-    const long most = keys / (t ? 4 * kChunkT : 2 * kStep * kRowsNW);
+    const long most = keys / (tiled(a, shared, elem_bytes) ? 8 * kChunkT : 8 * kStep);
     if (s > most) s = most;
-    return (int)(s < 1 ? 1 : s > 32 ? 32 : s);
+    return (int)(s < 1 ? 1 : s > kMaxParts ? kMaxParts : s);
   };
-  long keys = a.max_kv - a.prefix;
-  if (a.window > 0 && keys > (long)a.window + a.sinks + a.max_rows) keys = (long)a.window + a.sinks + a.max_rows;
-  p.splits = pick(false, keys);
-  if (a.prefix > 0) p.shared = pick(true, a.prefix);
+  p.splits = pick(false, keys_of(a, apart ? a.prefix : 0));
+  if (apart) p.shared = pick(true, a.prefix);
   return p;
 }
 
 size_t paged_part_floats(const PagedAttnArgs& a, const PagedPlan& p, size_t* ml) {
-  const size_t rows = p.z() > 1 ? (size_t)p.z() * a.r.n_rows * a.r.n_q_heads : 0;
+  const size_t rows = (size_t)p.parts() * a.r.n_rows * a.r.n_q_heads;
   *ml = rows * 2;
   return rows * a.r.head_dim;
 }
@@ -729,26 +868,38 @@ size_t paged_part_floats(const PagedAttnArgs& a, const PagedPlan& p, size_t* ml)
 template <typename T, int HD>
 static hipError_t attention_hd(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
   const PagedRows& r = a.r;
-  auto launch = [&](bool shared, int splits, int z0) {
-    const bool t = tiled(a, shared, sizeof(T));
-    const long grid = row_blocks(a, shared, t ? kTileRows : 16 * kRowsNT) * splits * r.n_kv_heads;
+  auto launch = [&](const PagedPass& ps) {
+    const bool t = tiled(a, ps.shared, sizeof(T));
+    const int nt = rows_nt(a, ps.shared, sizeof(T));
+    const long blocks = row_blocks(a, ps.shared, block_size(a, ps.shared, sizeof(T)));
+    const long grid = blocks * ps.splits * r.n_kv_heads;
     if (grid <= 0) return hipSuccess;
     if (grid > 0x7fffffffl) return hipErrorInvalidValue;
+    const dim3 gd((unsigned)grid);
     if constexpr (sizeof(T) == 2) {
       if (t) {
-        RT_LAUNCH((paged_tile_kernel<HD>), dim3((unsigned)grid), dim3(256), 0, s, a, shared ? 1 : 0, splits, z0, p.z());
+        // a workgroup that has a compute unit to itself takes twice the stages
+        if (grid <= 256) RT_LAUNCH((paged_tile_kernel<HD, 4>), gd, dim3(256), 0, s, a, ps);
+        else RT_LAUNCH((paged_tile_kernel<HD, 2>), gd, dim3(256), 0, s, a, ps);
+        return hipGetLastError();
+      }
+    } else if constexpr (HD == 64) {
+      if (nt == 2) {
+        RT_LAUNCH((paged_rows_kernel<T, HD, 2, 4, false>), gd, dim3(256), 0, s, a, ps);
         return hipGetLastError();
       }
     }
-    RT_LAUNCH((paged_rows_kernel<T, HD, kRowsNT, kRowsNW>), dim3((unsigned)grid), dim3(64 * kRowsNW), 0, s, a,
-              shared ? 1 : 0, splits, z0, p.z());
+    if (streamed(a, ps.first, sizeof(T))) RT_LAUNCH((paged_rows_kernel<T, HD, 1, 4, true>), gd, dim3(256), 0, s, a, ps);
+    else RT_LAUNCH((paged_rows_kernel<T, HD, 1, 4, false>), gd, dim3(256), 0, s, a, ps);
     return hipGetLastError();
   };
-  hipError_t e = p.shared ? launch(true, p.shared, p.splits) : hipSuccess;
-  if (e == hipSuccess) e = launch(false, p.splits, 0);
-  if (e != hipSuccess || p.z() == 1) return e;
+  hipError_t e = hipSuccess;
+  if (p.shared) e = launch(PagedPass{1, 0, p.shared, 0, 0});
+  const bool done = p.splits == 1;
+  if (e == hipSuccess) e = launch(PagedPass{0, p.shared ? a.prefix : 0, p.splits, done ? -1 : p.shared, done ? p.shared : 0});
+  if (e != hipSuccess || done) return e;
   const long rows = (long)r.n_rows * r.n_q_heads;
-  RT_LAUNCH((paged_merge_kernel<T, HD>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p.z());
+  RT_LAUNCH((paged_merge_kernel<T, HD>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p.parts());
   return hipGetLastError();
 }
 template <typename T>

@@ -15,6 +15,7 @@ import torch
 from . import binding as B
 
 PAGE = 16
+_lib = B._lib
 _DTYPES = {torch.bfloat16: B.RT_BF16, torch.float32: B.RT_F32}
 
 
@@ -37,37 +38,41 @@ class PagedKV:
             raise _invalid("k and v are bfloat16 or float32, the page table int32")
         if not (k.is_contiguous() and v.is_contiguous() and page_table.is_contiguous()):
             raise _invalid("k, v and the page table must be contiguous")
-        _on(k.device, v=v, page_table=page_table)
         self.k, self.v, self.page_table = k, v, page_table
         self.device, self.dtype = k.device, k.dtype
-        self.n_kv_heads, self.head_dim = h, d
+        self.index = k.get_device()          # -1: not on a GPU
+        self.n_kv_heads, self.head_dim, self.n_tables = h, d, page_table.shape[0]
+        _on(self, v, page_table)
         self.desc = B.rt_paged_kv(k.data_ptr(), v.data_ptr(), page_table.data_ptr(), n, page_table.shape[1], h, d,
                                   PAGE, _DTYPES[k.dtype])
 
 
-def _on(device: torch.device, **tensors) -> None:
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise _invalid(f"{name} is on {t.device}, the cache on {device}")
+# (The checks below run on every call of a decoding step, so they are written flat.)
+
+def _on(cache: PagedKV, *tensors) -> None:
+    for t in tensors:
+        if t is not None and t.get_device() != cache.index:
+            raise _invalid(f"a tensor is on {t.device}, the cache on {cache.device}")
 
 
-def _rows(name: str, t: torch.Tensor, head_dim: int) -> int:
+def _row_stride(name: str, t: torch.Tensor, head_dim: int) -> int:
     """Row stride of [rows][heads][head_dim] whose heads lie one after the other."""
-    if t.dim() != 3 or t.shape[2] != head_dim:
+    st = t.stride()
+    if len(st) != 3 or t.shape[2] != head_dim:
         raise _invalid(f"{name} is [rows][heads][{head_dim}], not {tuple(t.shape)}")
-    if (t.stride(2) != 1 or t.stride(1) != head_dim) and t.numel():
+    if (st[2] != 1 or st[1] != head_dim) and t.numel():
         raise _invalid(f"the heads of a row of {name} must lie one after the other")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * head_dim
+    return st[0] if t.shape[0] > 1 else t.shape[1] * head_dim
 
 
 def _seqs(cache: PagedKV, kv_len: torch.Tensor, row_start: Optional[torch.Tensor]) -> int:
-    n = kv_len.shape[0]
-    if kv_len.dim() != 1 or kv_len.dtype != torch.int32 or not kv_len.is_contiguous():
+    if kv_len.dtype is not torch.int32 or kv_len.dim() != 1 or not kv_len.is_contiguous():
         raise _invalid("kv_len is a contiguous int32 vector")
-    if n > cache.page_table.shape[0]:
+    n = kv_len.shape[0]
+    if n > cache.n_tables:
         raise _invalid("more sequences than rows of the page table")
-    if row_start is not None and (row_start.dtype != torch.int32 or tuple(row_start.shape) != (n + 1,)
-                                  or not row_start.is_contiguous()):
+    if row_start is not None and (row_start.dtype is not torch.int32 or row_start.dim() != 1
+                                  or row_start.shape[0] != n + 1 or not row_start.is_contiguous()):
         raise _invalid("row_start is a contiguous int32 vector of one more entry than kv_len")
     return n
 
@@ -76,23 +81,18 @@ def _ptr(t: Optional[torch.Tensor]) -> int:
     return 0 if t is None else t.data_ptr()
 
 
-class _Stream:
-    """The current stream of a device, with that device current."""
-
-    def __init__(self, device: torch.device):
-        if device.type != "cuda":
-            raise _invalid(f"the cache is on {device}, not on a GPU")
-        self.guard = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
-        self.device = device
-
-    def __enter__(self) -> int:
-        if self.guard:
-            self.guard.__enter__()
-        return torch.cuda.current_stream(self.device).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard:
-            self.guard.__exit__(*exc)
+def _launch(cache: PagedKV, call, *args) -> None:
+    """call(*args, the current stream of the cache's device), with that device current."""
+    index = cache.index
+    if index < 0:
+        raise _invalid(f"the cache is on {cache.device}, not on a GPU")
+    if torch.cuda.current_device() == index:
+        status = call(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            status = call(*args, torch._C._cuda_getCurrentRawStream(index))
+    if status != B.RT_OK:
+        raise B.RetraceError(status, B.rt_last_error())
 
 
 def rope_table(theta: float, rot_dim: int, positions: int, device) -> torch.Tensor:
@@ -115,21 +115,20 @@ def kv_append(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, kv_len: torch.Te
     are skipped (of no sequence, or at positions outside the page table) are left as they are in
     q_out, and hold anything in a q_out made here."""
     n, hd = _seqs(cache, kv_len, row_start), cache.head_dim
-    _on(cache.device, k=k, v=v, kv_len=kv_len, row_start=row_start, q=q, q_out=q_out, rope=rope, q_norm=q_norm,
-        k_norm=k_norm)
+    _on(cache, k, v, kv_len, row_start, q, q_out, rope, q_norm, k_norm)
     src, rows = k.dtype, k.shape[0]
-    if src not in _DTYPES or v.dtype != src or (q is not None and q.dtype != src):
+    if src not in _DTYPES or v.dtype is not src or (q is not None and q.dtype is not src):
         raise _invalid("q, k and v have one dtype, bfloat16 or float32")
-    ldk, ldv, ldq, ldqo, hq = _rows("k", k, hd), _rows("v", v, hd), 0, 0, 0
+    ldk, ldv, ldq, ldqo, hq = _row_stride("k", k, hd), _row_stride("v", v, hd), 0, 0, 0
     if k.shape[1] != cache.n_kv_heads or v.shape != k.shape:
         raise _invalid("k and v have the cache's heads and the same rows")
     if q is not None:
-        ldq, hq = _rows("q", q, hd), q.shape[1]
+        ldq, hq = _row_stride("q", q, hd), q.shape[1]
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=cache.dtype, device=cache.device)
         if q.shape[0] != rows or q_out.shape != q.shape or q_out.dtype != cache.dtype:
             raise _invalid("q has the rows of k, and q_out the shape of q and the cache's dtype")
-        ldqo = _rows("q_out", q_out, hd)
+        ldqo = _row_stride("q_out", q_out, hd)
     elif q_out is not None:
         raise _invalid("q_out without q")
     positions = rot = 0
@@ -143,30 +142,36 @@ def kv_append(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, kv_len: torch.Te
     args = B.rt_append_args(_ptr(q), k.data_ptr(), v.data_ptr(), ldq, ldk, ldv, _ptr(q_out), ldqo, _ptr(row_start),
                             kv_len.data_ptr(), _ptr(rope), _ptr(q_norm), _ptr(k_norm), _DTYPES[src], n, rows, hq,
                             positions, rot, eps)
-    with _Stream(cache.device) as s:
-        B.rt_kv_append(cache.desc, args, s)
+    _launch(cache, _lib.rt_kv_append, cache.desc, args)
     return q_out
 
 
 def _attention(call, cache, q, kv_len, window, sinks, prefix_len, row_start, max_rows, max_kv, scale, out, workspace):
     n = _seqs(cache, kv_len, row_start)
-    _on(cache.device, q=q, kv_len=kv_len, row_start=row_start, out=out, workspace=workspace)
-    ldq = _rows("q", q, cache.head_dim)
-    if q.dtype != cache.dtype:
+    _on(cache, q, kv_len, row_start, out, workspace)
+    ldq = _row_stride("q", q, cache.head_dim)
+    if q.dtype is not cache.dtype:
         raise _invalid("q has the cache's dtype")
+    rows, heads, _ = q.shape
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape or out.dtype != q.dtype:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        ldo = heads * cache.head_dim
+    elif out.shape != q.shape or out.dtype is not cache.dtype:
         raise _invalid("out has the shape and dtype of q")
-    args = B.rt_attn_args(q.data_ptr(), ldq, out.data_ptr(), _rows("out", out, cache.head_dim), _ptr(row_start),
-                          kv_len.data_ptr(), n, q.shape[0], q.shape[1], max_rows, max_kv, window, sinks, prefix_len,
-                          scale)
-    with _Stream(cache.device) as s:
-        need = B.rt_attn_workspace_bytes(cache.desc, args)
-        if workspace is None and need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
-        call(cache.desc, args, _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-             s)
+    else:
+        ldo = _row_stride("out", out, cache.head_dim)
+    args = B.rt_attn_args(q.data_ptr(), ldq, out.data_ptr(), ldo, _ptr(row_start), kv_len.data_ptr(), n, rows, heads,
+                          max_rows, max_kv, window, sinks, prefix_len, scale)
+    desc = cache.desc
+    if workspace is not None:
+        _launch(cache, call, desc, args, workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        return out
+    need = _lib.rt_attn_workspace_bytes(desc, args)
+    if need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
+        _launch(cache, call, desc, args, workspace.data_ptr(), need)
+    else:
+        _launch(cache, call, desc, args, 0, 0)
     return out
 
 
@@ -178,7 +183,7 @@ def window_attention(cache: PagedKV, q: torch.Tensor, kv_len: torch.Tensor, wind
     positions j <= p with j > p - window or j < sinks.  See rt_window_attention.  The workspace is
     allocated where none is given.  Rows of no sequence are left as they are in out, and hold
     anything in an out made here."""
-    return _attention(B.rt_window_attention, cache, q, kv_len, window, sinks, 0, row_start, max_rows, max_kv, scale,
+    return _attention(_lib.rt_window_attention, cache, q, kv_len, window, sinks, 0, row_start, max_rows, max_kv, scale,
                       out, workspace)
 
 
@@ -189,5 +194,5 @@ def prefix_attention(cache: PagedKV, q: torch.Tensor, kv_len: torch.Tensor, pref
     """Causal attention of the rows q over the cache, whose sequences share the pages of their first
     prefix_len positions: those are read once for the batch.  See rt_prefix_attention; workspace and
     out as for window_attention."""
-    return _attention(B.rt_prefix_attention, cache, q, kv_len, 0, 0, prefix_len, row_start, max_rows, max_kv, scale,
+    return _attention(_lib.rt_prefix_attention, cache, q, kv_len, 0, 0, prefix_len, row_start, max_rows, max_kv, scale,
                       out, workspace)

@@ -375,3 +375,35 @@ def test_two_streams_at_once(ops):
     torch.cuda.synchronize()
     for a, b in got:
         assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+
+
+@pytest.mark.parametrize("heads,dtype,seqs,prefix,rows", [
+    ((8, 8, 128), BF, 40, 512, [1]), ((40, 8, 128), BF, 33, 528, [1]), ((16, 8, 64), BF, 60, 1024, [3]),
+    ((16, 8, 128), BF, 24, 1040, [0, 1, 5, 16]), ((4, 4, 64), F32, 64, 512, [1]), ((8, 4, 128), F32, 30, 800, [2]),
+    ((6, 2, 64), F32, 64, 1040, [0, 1, 2, 9])], ids=repr)
+def test_prefix_in_a_pass_of_its_own(ops, heads, dtype, seqs, prefix, rows):
+    """Batches that make the prefix pass worth its launch (the workspace holds its parts)."""
+    rows = [rows[i % len(rows)] for i in range(seqs)]
+    keys = [prefix + r + (11 * i) % 70 for i, r in enumerate(rows)]
+    keys[3] = prefix - 20 + rows[3]                        # one of the sequences ends inside the prefix
+    c = Case(rows, keys, heads, dtype, seed=seqs, extra_rows=2, shared=prefix)
+    c.table[3, :prefix // PAGE] = c.table[0, :prefix // PAGE]
+    assert workspace_bytes(ops, c, prefix) > 0
+    out = torch.full((c.n, c.hq, c.hd), 7.0, dtype=dtype, device=DEV)
+    check(attend(ops, c, prefix=prefix, out=out, max_kv=max(keys)), *ref_attention(c))
+    assert (out[-2:] == 7).all()
+
+
+@pytest.mark.parametrize("heads,dtype,rows", [((8, 8, 128), BF, 1), ((16, 8, 64), BF, 16), ((4, 4, 64), F32, 2)], ids=repr)
+def test_prefix_pass_and_splits_of_the_rest(ops, heads, dtype, rows):
+    """Long sequences of their own behind a long prefix: parts of both meet in the merge."""
+    prefix, S = 2048, 14
+    c = Case([rows] * S, [prefix + rows + 300 * i for i in range(S)], heads, dtype, seed=1, ragged=False, shared=prefix)
+    check(attend(ops, c, prefix=prefix, max_kv=max(c.keys)), *ref_attention(c))
+
+
+def workspace_bytes(ops, c, prefix):
+    from paper_2608_29748_amd import binding as B
+    kv = B.rt_paged_kv(1 << 20, 1 << 20, 1 << 20, c.n_pages, c.width, c.hkv, c.hd, 16, 1 if c.dtype == BF else 0)
+    return B.rt_attn_workspace_bytes(kv, B.rt_attn_args(0, 0, 0, 0, 1 << 20, 1 << 20, len(c.rows), c.n, c.hq, max(c.rows),
+                                                        max(c.keys), 0, 0, prefix, 0.0))
