@@ -148,6 +148,22 @@ int rt_init_models(const rt_config* cfg, const void* const* weights, int32_t n_w
 int rt_prefill(rt_model* m, int32_t n_seqs, const int32_t* prompt_lens, const int32_t* prompt_ids,
                int32_t gen_budget, int32_t* first_tokens);
 
+/* rt_prefill for prompts that begin with the same prefix_len tokens (host): sequence s has the
+ * prompt prefix_ids followed by its prompt_lens[s] (at least 1) own tokens of prompt_ids.  Same
+ * meaning as rt_prefill of those prompts, with the prefix computed and kept once: the sequences'
+ * page tables share the pages that it fills (16 tokens each; what is left of it is each sequence's own),
+ * and rounds and target-only steps read those once for the batch where that pays
+ * (rt_prefix_attention).  The next rt_prefill unshares them.  prefix_len + prompt_len + gen_budget +
+ * block_size must not exceed max_seq_len. */
+int rt_prefill_prefix(rt_model* m, int32_t prefix_len, const int32_t* prefix_ids, int32_t n_seqs,
+                      const int32_t* prompt_lens, const int32_t* prompt_ids, int32_t gen_budget, int32_t* first_tokens);
+
+/* Gives the target's attention a sliding window with sinks, in every layer: a row sees the last
+ * `window` positions, its own included, and the first `sinks` ones (rt_window_attention).  window 0
+ * (with sinks 0; the initial state): every position.  The drafter's attention keeps its full context.
+ * Holds for the prompts too, so the next call must be a prefill (RT_ERR_STATE otherwise). */
+int rt_set_window(rt_model* m, int32_t window, int32_t sinks);
+
 /* One ReTrace round for every prefilled sequence.  Outputs (host):
  *   tokens[n_seqs][block_size]: committed tokens of this round, the first
  *     n_committed[s] entries valid (accepted drafts, then the target's correction

@@ -71,15 +71,18 @@ def apply_rope(x: np.ndarray, positions: np.ndarray, theta: float) -> np.ndarray
 
 
 def attention(q: np.ndarray, k: np.ndarray, v: np.ndarray, q_pos: np.ndarray,
-              k_pos: np.ndarray, causal: bool) -> np.ndarray:
+              k_pos: np.ndarray, causal: bool, window: int = 0, sinks: int = 0) -> np.ndarray:
     """Grouped-query softmax attention.  q[n, Hq, hd], k/v[T, Hkv, hd]; query head h
     reads kv head h // (Hq/Hkv).  causal: key position must not exceed the query's.
+    window > 0: nor lie `window` or more before it, unless it is below `sinks`.
     The probabilities are the plain softmax of the scaled scores (no storage rounding:
     only the stored output is rounded)."""
     n, hq, hd = q.shape
     group = hq // k.shape[1]
     out = np.empty_like(q)
     visible = (k_pos[None, :] <= q_pos[:, None]) if causal else np.ones((n, len(k_pos)), bool)
+    if window > 0:
+        visible &= (k_pos[None, :] > q_pos[:, None] - window) | (k_pos[None, :] < sinks)
     for h in range(hq):
         kh = h // group
         s = (q[:, h, :] @ k[:, kh, :].T) / np.sqrt(hd)
@@ -167,8 +170,9 @@ class VerifyOut:
 
 class OracleModel:
     def __init__(self, wl: Workload, stored: Dict[str, np.ndarray],
-                 prec: Optional[Precision] = None, cache=True):
+                 prec: Optional[Precision] = None, cache=True, window: int = 0, sinks: int = 0):
         self.wl = wl
+        self.window, self.sinks = window, sinks      # of the target's (causal) attention
         self.s = wl.target
         self.W = Weights(stored, cache)
         self.prec = prec or Precision.for_dtype(wl.dtype)
@@ -190,7 +194,8 @@ class OracleModel:
     # -- the rest of a decoder layer, one storage point per step
     def attn_out(self, q, keys, vals, q_pos, k_pos, causal: bool) -> np.ndarray:
         """Attention output rows [n][Hq*hd], rounded to the storage type."""
-        return self.prec.a(attention(q, keys, vals, q_pos, k_pos, causal)).reshape(q.shape[0], -1)
+        window = self.window if causal else 0
+        return self.prec.a(attention(q, keys, vals, q_pos, k_pos, causal, window, self.sinks)).reshape(q.shape[0], -1)
 
     def o_residual(self, pre: str, x, o) -> np.ndarray:
         """Residual after the attention block: x + o W_o^T."""

@@ -48,7 +48,8 @@ EXPORTS = ["rt_workspace_bytes", "rt_weight_count", "rt_init_models", "rt_prefil
            "rt_destroy", "rt_last_error", "rt_set_debug", "rt_spec_round_forced", "rt_debug_read",
            "rt_debug_write", "rt_profile_round", "rt_time_kernel", "rt_ar_steps", "rt_debug_read_rows",
            "rt_spec_round_static", "rt_stream_read", "rt_weight_elements", "rt_debug_choice",
-           "rt_kv_append", "rt_attn_workspace_bytes", "rt_window_attention", "rt_prefix_attention"]
+           "rt_kv_append", "rt_attn_workspace_bytes", "rt_window_attention", "rt_prefix_attention",
+           "rt_prefill_prefix", "rt_set_window"]
 
 
 class RetraceError(RuntimeError):
@@ -119,6 +120,8 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.rt_init_models.argtypes = [C.POINTER(rt_config), C.POINTER(P), C.c_int32, P, C.c_size_t, P,
                                    C.POINTER(P)]
     lib.rt_prefill.argtypes = [P, C.c_int32, i32p, i32p, C.c_int32, i32p]
+    lib.rt_prefill_prefix.argtypes = [P, C.c_int32, i32p, C.c_int32, i32p, i32p, C.c_int32, i32p]
+    lib.rt_set_window.argtypes = [P, C.c_int32, C.c_int32]
     lib.rt_spec_round.argtypes = [P, i32p, i32p, i32p]
     lib.rt_spec_round_forced.argtypes = [P, i32p, i32p, i32p, i32p]
     lib.rt_spec_round_static.argtypes = [P, P, P, P]
@@ -144,7 +147,7 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
                  "rt_stream_read", "rt_destroy",
                  "rt_set_debug", "rt_debug_read", "rt_debug_read_rows", "rt_debug_write", "rt_profile_round",
                  "rt_time_kernel", "rt_ar_steps", "rt_debug_choice", "rt_kv_append", "rt_window_attention",
-                 "rt_prefix_attention"):
+                 "rt_prefix_attention", "rt_prefill_prefix", "rt_set_window"):
         getattr(lib, name).restype = C.c_int
     return lib
 
@@ -205,6 +208,21 @@ def rt_prefill(h: int, prompts: Sequence[np.ndarray], gen_budget: int) -> np.nda
     _check(_lib.rt_prefill(C.c_void_p(h), len(prompts), lp, ip, gen_budget,
                            first.ctypes.data_as(C.POINTER(C.c_int32))))
     return first
+
+
+def rt_prefill_prefix(h: int, prefix: np.ndarray, prompts: Sequence[np.ndarray], gen_budget: int) -> np.ndarray:
+    """rt_prefill of prefix + prompt for every prompt, the prefix computed and kept once."""
+    pre, pp = _i32(prefix)
+    lens, lp = _i32([len(p) for p in prompts])
+    ids, ip = _i32(np.concatenate([np.asarray(p) for p in prompts]) if len(prompts) else [])
+    first = np.zeros(len(prompts), np.int32)
+    _check(_lib.rt_prefill_prefix(C.c_void_p(h), len(pre), pp, len(prompts), lp, ip, gen_budget,
+                                  first.ctypes.data_as(C.POINTER(C.c_int32))))
+    return first
+
+
+def rt_set_window(h: int, window: int, sinks: int = 0) -> None:
+    _check(_lib.rt_set_window(C.c_void_p(h), window, sinks))
 
 
 def rt_spec_round(h: int, n_seqs: int, block_size: int):

@@ -13,6 +13,7 @@
 #include "gemm.h"
 #include "host.h"
 #include "misc.h"
+#include "paged.h"
 #include "sample.h"
 
 namespace rt {
@@ -76,6 +77,9 @@ struct EngineBase {
   bool own_stream = false;
   int n_seqs = 0;
   bool prefilled = false;
+  int window = 0, sinks = 0;     // of the target's attention (window 0: full), see rt_set_window
+  int shared = 0;                // positions whose pages the sequences share (rt_prefill_prefix)
+  std::vector<int32_t> h_pages;  // page table as uploaded
   int flags = 0;
   hipGraph_t graph = nullptr;
   hipGraphExec_t gexec = nullptr;
@@ -196,7 +200,7 @@ struct EngineBase {
   }
   template <class X> X* at(size_t off) const { return reinterpret_cast<X*>(ws + off); }
   virtual int init(const void* const* w) = 0;
-  virtual int prefill(int ns, const int32_t* lens, const int32_t* ids, int budget, int32_t* first) = 0;
+  virtual int prefill(int ns, const int32_t* lens, const int32_t* ids, int budget, int share, int32_t* first) = 0;
   virtual int run_round(bool forced) = 0;
   virtual int run_ar_step() = 0;
   int read_outputs(int32_t* tokens, int32_t* n_comm, int32_t* acc);
@@ -361,6 +365,14 @@ struct Engine : EngineBase {
     int n_blocks = 0;
     const int32_t* items = nullptr;
     int n_items = 0;
+    // attention over the cache by the paged operators: a window (target layers), or a prefix
+    // whose pages the sequences share
+    int window = 0, sinks = 0, prefix = 0;
+    // prompt pass with a window: its segments, one of each of n_segs consecutive sequences from
+    // sequence seg0 on (row offsets in the pass, n_segs + 1 of them; keys up to the segment's end)
+    const int32_t* seg_start = nullptr;
+    const int32_t* seg_keys = nullptr;
+    int seg0 = 0, n_segs = 0, seg_rows = 0, seg_kv = 0;
   };
   // partials of the last deferred residual GEMM, consumed by the next norm of x
   NormFold pend{};
@@ -403,6 +415,78 @@ struct Engine : EngineBase {
     return gemm_call(kind, A, lda, q.Mrows, false, W, q.d, Kp, c.M, e, k_logical);
   }
 
+  // Whether a layer's attention is the paged operators': with a window, or where a pass of its own
+  // over the shared prefix pays.  Then their arguments and plan.
+  bool paged_layer(const LayerCtx& c, PagedAttnArgs* out, PagedPlan* plan) const {
+    const Plan& q = p;
+    if (c.window <= 0 && (c.prefix <= 0 || c.blocks)) return false;
+    PagedAttnArgs a{};
+    PagedRows& r = a.r;
+    r.k = c.kc; r.v = c.vc; r.max_pages = q.pages_per_seq; r.n_pages = q.n_pages;
+    r.page_table = c.pt + (size_t)c.seg0 * q.pages_per_seq;
+    r.n_q_heads = q.Hq; r.n_kv_heads = q.Hkv; r.head_dim = q.hd; r.n_rows = c.M;
+    if (c.blocks) {
+      r.n_seqs = c.n_segs; r.row_start = c.seg_start; r.kv_len = c.seg_keys; r.kv_stride = 1;
+      a.max_rows = c.seg_rows; a.max_kv = c.seg_kv;
+    } else {
+      r.n_seqs = c.n_seqs; r.rows_each = c.rows_per_seq;
+      r.kv_len = c.pos0; r.kv_stride = c.stride; r.kv_add = c.rows_per_seq;
+      a.max_rows = c.rows_per_seq; a.max_kv = q.T;
+    }
+    a.q = at<T>(q.qbuf); a.ldq = q.qN; a.out = at<T>(q.attn); a.ldo = 16 * q.Kp_q; a.packed = 1;
+    a.causal = c.causal; a.scale = 1.0f / sqrtf((float)q.hd);
+    a.window = c.window; a.sinks = c.sinks; a.prefix = c.window > 0 ? 0 : c.prefix;
+    a.part_o = pat<float>(q.opart, q.s_opart); a.part_ml = pat<float>(q.mlpart, q.s_mlpart);
+    PagedPlan pl = paged_plan(a, sizeof(T));
+    if (c.window <= 0 && pl.shared == 0) return false;
+    // (one part always fits: the buffer has a full set of rows for every split of the other kernels)
+    const size_t cap = (q.mlpart - q.opart) / 4, cap_ml = (q.attn_plan - q.mlpart) / 4;
+    size_t ml;
+    while (paged_part_floats(a, pl, &ml) > cap || ml > cap_ml) {
+      if (pl.splits > 1) --pl.splits;
+      else if (pl.shared > 1) --pl.shared;
+      else return false;
+    }
+    *out = a;
+    *plan = pl;
+    return true;
+  }
+  // The rows' keys and values into the cache, their queries into qbuf, and the attention output.
+  int paged_attn(const char* lw, const LayerCtx& c, const PagedAttnArgs& a, const PagedPlan& pl) {
+    const Plan& q = p;
+    AppendArgs g{};
+    g.r = a.r;
+    g.q = at<float>(q.qkvf); g.ks = at<float>(q.qkvf) + q.qN; g.vs = at<float>(q.qkvf) + q.qN + q.kvN;
+    g.ldq = g.ldk = g.ldv = q.qkvN; g.q_out = at<T>(q.qbuf); g.ldqo = q.qN;
+    g.cos = at<float>(q.rope); g.sin = g.cos + (size_t)q.T * (q.hd / 2); g.rot_dim = q.hd;
+    g.q_norm = lw + q.lo_qn; g.k_norm = lw + q.lo_kn; g.eps = cfg.rms_eps;
+    prof_begin(RT_K_QKV_POST, (double)c.M * q.qkvN * (4 + sizeof(T)), 0);
+    HIPCHK((paged_append<T, float>(g, stream)));
+    prof_end();
+    CHK(trace_item(c.trace, TI_Q, at<T>(q.qbuf)));
+    if (c.blocks && c.n_blocks == 0) return RT_OK;      // (the last layer of prompts that do not end in this pass)
+    for (int i = 0; i < pl.launches(); ++i) {
+      double bytes = 0, flops = 0;
+      const bool pass = i < pl.passes(), pre = pl.shared && i == 0;
+      if (instrumented()) {   // (prompt passes are not instrumented)
+        const double E = sizeof(T), rows = (double)c.n_seqs * c.rows_per_seq;
+        double keys = pre ? a.prefix : 0;
+        for (int s = 0; s < c.n_seqs && !pre; ++s) {
+          const double n = c.prof_ctx[s] + c.rows_per_seq - (pl.shared ? a.prefix : 0);
+          keys += a.window > 0 ? fmin(n, (double)a.window + a.sinks + c.rows_per_seq - 1) : n;
+        }
+        const double part = rows * q.Hq * (q.hd + 2) * 4.0;
+        bytes = pass ? keys * 2.0 * q.Hkv * q.hd * E + rows * q.qN * E : part * pl.parts();
+        if (pass) bytes += pre ? part * pl.shared : pl.splits > 1 ? part * pl.splits : part * pl.shared + rows * q.qN * E;
+        flops = pass ? 4.0 * keys * (pre ? rows : c.rows_per_seq) * q.Hq * q.hd : 0;
+      }
+      prof_begin(pass ? RT_K_ATTENTION : RT_K_ATTN_MERGE, bytes, flops);
+      HIPCHK(paged_launch<T>(a, pl, i, stream));
+      prof_end();
+    }
+    return trace_item(c.trace, TI_ATTN, at<T>(q.attn));
+  }
+
   // First half of a decoder layer: input norm, q|k|v, K / V cache rows, attention output.
   int layer_attn(const char* lw, const LayerCtx& c) {
     const Plan& q = p;
@@ -412,7 +496,10 @@ struct Engine : EngineBase {
     CHK(trace_item(c.trace, TI_X, x));   // the norm has folded any deferred partials into x
     // q|k|v on the mid-size kernel with k slabs: the slabs go to the split buffer and
     // qkv_post adds them (in slab order, as the slab epilogue would) while reading
-    const int qks = qkv_slabs(c.M);
+    PagedAttnArgs pa;
+    PagedPlan pplan;
+    const bool paged = paged_layer(c, &pa, &pplan);
+    const int qks = paged ? 1 : qkv_slabs(c.M);
     EpiArgs e{};
     if (qks > 1) {
       e.kind = EPI_PARTIAL; e.out_f32 = pat<float>(q.partial, q.s_partial); e.ldo = q.qkvN;
@@ -421,6 +508,7 @@ struct Engine : EngineBase {
       e.kind = EPI_STORE_F32; e.out_f32 = at<float>(q.qkvf); e.ldo = q.qkvN;
     }
     CHK(gemm_call(RT_K_GEMM_QKV, xa, 16 * q.Kp_d, q.Mrows, false, lw + q.lo_qkv, q.qkvN, q.Kp_d, c.M, e, q.d, qks));
+    if (paged) return paged_attn(lw, c, pa, pplan);
     // Rounds and target-only steps (at most 16 rows per sequence, bf16, one q|k|v slab):
     // the attention kernel does the q / k-norm, the rotation and the block's K / V cache
     // write itself (debug flag 16 keeps the separate kernel)
@@ -650,11 +738,7 @@ struct Engine : EngineBase {
       lowrank_gate_bias<T>(W(b3 + 3), at<T>(q.embed), q.d, cfg.mask_token_id, at<float>(q.lr_ge), stream);
     }
     HIPCHK(hipGetLastError());
-    // page table: page j of sequence s is pool page j * max_batch + s
-    std::vector<int32_t> pt((size_t)q.n_pages);
-    for (int s = 0; s < q.bmax; ++s)
-      for (int j = 0; j < q.pages_per_seq; ++j) pt[(size_t)s * q.pages_per_seq + j] = j * q.bmax + s;
-    HIPCHK(hipMemcpyAsync(ws + q.page_table, pt.data(), pt.size() * 4, hipMemcpyHostToDevice, stream));
+    CHK(upload_pages(0));
     // RoPE table: angle = fp32(pos * fp32(theta^(-2i/hd))); cos and sin rounded to fp32
     const int half = q.hd / 2;
     std::vector<float> rope((size_t)q.T * half * 2);
@@ -671,13 +755,30 @@ struct Engine : EngineBase {
     return RT_OK;
   }
 
+  // Page table: page j of sequence s is pool page j * max_batch + s; the first `share` positions (a
+  // multiple of 16) of every sequence lie in the pages of sequence 0.
+  int upload_pages(int share) {
+    const Plan& q = p;
+    h_pages.resize((size_t)q.n_pages);
+    for (int s = 0; s < q.bmax; ++s)
+      for (int j = 0; j < q.pages_per_seq; ++j)
+        h_pages[(size_t)s * q.pages_per_seq + j] = j * q.bmax + (j < share / kPage ? 0 : s);
+    HIPCHK(hipMemcpyAsync(ws + q.page_table, h_pages.data(), h_pages.size() * 4, hipMemcpyHostToDevice, stream));
+    return RT_OK;
+  }
+
   // Prompt tables of one prefill, as uploaded to pf_tab: the prompts' tokens laid end to
   // end, each sequence's first token index (n_seqs + 1 offsets), and per pass the attention
-  // blocks, page items and the attention blocks of the ending sequences' last rows (int32
-  // offsets into the table).
-  struct PromptPass { int g0, rows, first_end, n_end; size_t blocks, items, ends; int n_blocks, n_items, n_ends; };
+  // blocks, page items, the attention blocks of the ending sequences' last rows and the segments
+  // (row offsets, then keys up to each one's end) (int32 offsets into the table).  Sequences past
+  // the first start at position `share`: what lies before is sequence 0's.
+  struct PromptPass {
+    int g0, rows, first_end, n_end;
+    size_t blocks, items, ends, segs;
+    int n_blocks, n_items, n_ends, n_segs, seg_rows, seg_kv;
+  };
   struct PromptTables { std::vector<int32_t> tab; size_t off; std::vector<PromptPass> passes; };
-  void prompt_tables(int ns, const int32_t* lens, const int32_t* ids, PromptTables* out) const {
+  void prompt_tables(int ns, const int32_t* lens, const int32_t* ids, int share, PromptTables* out) const {
     const Plan& q = p;
     std::vector<int32_t> off(ns + 1, 0);
     for (int s = 0; s < ns; ++s) off[s + 1] = off[s] + lens[s];
@@ -690,6 +791,7 @@ struct Engine : EngineBase {
     const int rbr = sizeof(T) == 2 ? kAttnRowsPrompt : kAttnRows;
     struct Blk { int s, row, n, pos, rb, keys; };
     std::vector<Blk> blk;
+    std::vector<int32_t> seg_start, seg_keys;
     int s0 = 0;
     for (int g0 = 0; g0 < total; g0 += per) {
       PromptPass ps{};
@@ -699,12 +801,18 @@ struct Engine : EngineBase {
       while (off[s0 + 1] <= g0) ++s0;
       ps.first_end = s0;
       blk.clear();
+      seg_start.clear();
+      seg_keys.clear();
       t.resize(rup(t.size(), 4), 0);
       ps.items = t.size();
       for (int s = s0; s < ns && off[s] < g1; ++s) {
         const int b = off[s] > g0 ? off[s] : g0, e = off[s + 1] < g1 ? off[s + 1] : g1;
-        const int pos = b - off[s], n = e - b, row = b - g0;
+        const int pos = b - off[s] + (s > 0 ? share : 0), n = e - b, row = b - g0;
         if (e == off[s + 1]) ps.n_end += 1;
+        seg_start.push_back(row);
+        seg_keys.push_back(pos + n);
+        ps.seg_rows = n > ps.seg_rows ? n : ps.seg_rows;
+        ps.seg_kv = pos + n > ps.seg_kv ? pos + n : ps.seg_kv;
         for (int rb = 0; rb * rbr < n * q.G; ++rb) {
           const int last = (n * q.G < (rb + 1) * rbr ? n * q.G : (rb + 1) * rbr) - 1;
           blk.push_back(Blk{s, row, n, pos, rb, pos + last / q.G + 1});
@@ -730,22 +838,34 @@ struct Engine : EngineBase {
       // token's G rows may start in the block before, which then is listed too)
       ps.ends = t.size();
       for (const Blk& x : blk) {
-        const int end = x.pos + x.n == lens[x.s] ? x.n * q.G : 0;     // rows of an ending segment
+        const int end = x.pos + x.n == lens[x.s] + (x.s > 0 ? share : 0) ? x.n * q.G : 0;     // rows of an ending segment
         if (end > 0 && (x.rb + 1) * rbr > end - q.G) { put(x); ps.n_ends += 1; }
       }
+      ps.segs = t.size();
+      ps.n_segs = (int)seg_keys.size();
+      t.insert(t.end(), seg_start.begin(), seg_start.end());
+      t.push_back(ps.rows);
+      t.insert(t.end(), seg_keys.begin(), seg_keys.end());
       out->passes.push_back(ps);
     }
   }
 
   // The prompts' rows run in passes over all sequences together, so that every pass fills
   // the chip and streams the weights once.
-  int prefill(int ns, const int32_t* lens, const int32_t* ids, int budget, int32_t* first) override {
+  // share: positions (a multiple of 16) whose keys and values sequence 0 computes for all of them;
+  // lens and ids of the other sequences then hold what comes after.
+  int prefill(int ns, const int32_t* lens, const int32_t* ids, int budget, int share, int32_t* first) override {
     const Plan& q = p;
     prefilled = false;
     ar_mode = false;
     PromptTables pt;
-    prompt_tables(ns, lens, ids, &pt);
+    prompt_tables(ns, lens, ids, share, &pt);
     if (pt.tab.size() > q.pf_tab_ints) return fail(RT_ERR_CAPACITY, "prompt tables exceed their buffer");
+    if (share != shared) {
+      drop_graph();
+      CHK(upload_pages(share));
+      shared = share;
+    }
     HIPCHK(hipMemcpyAsync(ws + q.pf_tab, pt.tab.data(), pt.tab.size() * 4, hipMemcpyHostToDevice, stream));
     const int32_t* tab = at<int32_t>(q.pf_tab);
     const int32_t* off = tab + pt.off;
@@ -753,7 +873,7 @@ struct Engine : EngineBase {
     const int rbr = sizeof(T) == 2 ? kAttnRowsPrompt : kAttnRows;
     int rc = RT_OK;
     for (const PromptPass& ps : pt.passes) {
-      if ((rc = prompt_pass(ps, tab, off, ptab, rbr, budget)) != RT_OK) break;
+      if ((rc = prompt_pass(ps, tab, off, ptab, rbr, budget, share)) != RT_OK) break;
     }
     if (rc != RT_OK) {
       (void)hipStreamSynchronize(stream);   // the tables are copied before they go
@@ -797,7 +917,7 @@ struct Engine : EngineBase {
   }
 
   int prompt_pass(const PromptPass& ps, const int32_t* tab, const int32_t* off, const int32_t* ptab, int rbr,
-                  int budget) {
+                  int budget, int share) {
     const Plan& q = p;
     const int n = ps.rows;
     const int32_t* items = tab + ps.items;
@@ -814,6 +934,9 @@ struct Engine : EngineBase {
                  slot >= 0 ? at<T>(q.g) : nullptr, slot * q.d, nullptr, l + 1 < q.L};
       c.blocks = tab + ps.blocks; c.n_blocks = ps.n_blocks;
       c.items = items; c.n_items = ps.n_items;
+      c.window = window; c.sinks = sinks;
+      c.seg_start = tab + ps.segs; c.seg_keys = c.seg_start + ps.n_segs + 1;
+      c.seg0 = ps.first_end; c.n_segs = ps.n_segs; c.seg_rows = ps.seg_rows; c.seg_kv = ps.seg_kv;
       if (tail && l + 1 == q.L) {
         c.blocks = tab + ps.ends; c.n_blocks = ps.n_ends;
         CHK(tail_layer(tlayer(l), c, ps, off, last));
@@ -832,7 +955,7 @@ struct Engine : EngineBase {
         CHK(dists(at<float>(q.vlogits), ps.n_end, at<int32_t>(q.dist_ids_v), at<float>(q.dist_p_v), SAMPLE_FIRST,
                   ps.first_end, at<int32_t>(q.stok)));
       first_tokens(at<int32_t>(q.state), ps.first_end, ps.n_end, at<uint64_t>(q.tkeys),
-                   smp ? at<int32_t>(q.stok) : nullptr, off, budget, at<int32_t>(q.first_tok), stream);
+                   smp ? at<int32_t>(q.stok) : nullptr, off, share, budget, at<int32_t>(q.first_tok), stream);
     }
     HIPCHK(hipGetLastError());
     return RT_OK;
@@ -899,6 +1022,7 @@ struct Engine : EngineBase {
                  at<T>(q.dkc) + (size_t)l * q.cache_layer_elems, at<T>(q.dvc) + (size_t)l * q.cache_layer_elems,
                  nullptr, 0, prof_ctx.data(), 1};
       c.trace = l;
+      c.prefix = shared;
       CHK(layer(dlayer(l), c));
     }
     stage(2);
@@ -923,6 +1047,7 @@ struct Engine : EngineBase {
                  at<T>(q.kc) + (size_t)l * q.cache_layer_elems, at<T>(q.vc) + (size_t)l * q.cache_layer_elems,
                  slot >= 0 ? at<T>(q.g) : nullptr, slot * q.d, prof_ctx.data(), 1};
       c.trace = q.LD + l;
+      c.window = window; c.sinks = sinks; c.prefix = shared;
       CHK(layer(tlayer(l), c));
     }
     stage(4);
@@ -975,6 +1100,7 @@ struct Engine : EngineBase {
       LayerCtx c{M, 1, n_seqs, kStateFields, 1, q.ar_splits, q.ar_rb, kAttnRows, st + ST_SEQ_LEN, pt,
                  at<T>(q.kc) + (size_t)l * q.cache_layer_elems, at<T>(q.vc) + (size_t)l * q.cache_layer_elems,
                  nullptr, 0, prof_ctx.data(), 1};
+      c.window = window; c.sinks = sinks; c.prefix = shared;
       CHK(layer(tlayer(l), c));
     }
     norm_x(at<T>(q.t_final_norm), M, nullptr, 0);
@@ -1510,10 +1636,62 @@ int rt_prefill(rt_model* m, int32_t n_seqs, const int32_t* prompt_lens, const in
     }
     for (size_t i = 0; i < total; ++i)
       if (prompt_ids[i] < 0 || prompt_ids[i] >= e.p.V) return fail(RT_ERR_TOKEN, "prompt token %d out of range", prompt_ids[i]);
-    return e.prefill(n_seqs, prompt_lens, prompt_ids, gen_budget, first_tokens);
+    return e.prefill(n_seqs, prompt_lens, prompt_ids, gen_budget, 0, first_tokens);
   } catch (...) {
     return fail(RT_ERR_INVALID, "unexpected exception in rt_prefill");
   }
+}
+
+int rt_prefill_prefix(rt_model* m, int32_t prefix_len, const int32_t* prefix_ids, int32_t n_seqs,
+                      const int32_t* prompt_lens, const int32_t* prompt_ids, int32_t gen_budget, int32_t* first_tokens) {
+  try {
+    if (!m || !m->e) return fail(RT_ERR_INVALID, "null model");
+    EngineBase& e = *m->e;
+    if (!prefix_ids || !prompt_lens || !prompt_ids || !first_tokens) return fail(RT_ERR_INVALID, "null pointer argument");
+    if (n_seqs < 1 || n_seqs > e.p.bmax) return fail(RT_ERR_CAPACITY, "n_seqs %d outside [1, %d]", n_seqs, e.p.bmax);
+    if (prefix_len < 1) return fail(RT_ERR_INVALID, "the prefix is empty");
+    if (gen_budget < 1) return fail(RT_ERR_INVALID, "gen_budget must be >= 1");
+    size_t total = 0;
+    for (int s = 0; s < n_seqs; ++s) {
+      const int len = prompt_lens[s];
+      if (len < 1) return fail(RT_ERR_INVALID, "prompt %d is empty", s);
+      if ((long long)prefix_len + len + gen_budget + e.p.bk > e.p.T)
+        return fail(RT_ERR_CAPACITY, "prompt %d: prefix %d + length %d + budget %d + block %d exceeds max_seq_len %d", s,
+                    prefix_len, len, gen_budget, e.p.bk, e.p.T);
+      total += (size_t)len;
+    }
+    for (int i = 0; i < prefix_len; ++i)
+      if (prefix_ids[i] < 0 || prefix_ids[i] >= e.p.V) return fail(RT_ERR_TOKEN, "prefix token %d out of range", prefix_ids[i]);
+    for (size_t i = 0; i < total; ++i)
+      if (prompt_ids[i] < 0 || prompt_ids[i] >= e.p.V) return fail(RT_ERR_TOKEN, "prompt token %d out of range", prompt_ids[i]);
+    // sequence 0 takes the whole prefix, the others what its full pages leave of it
+    const int share = n_seqs > 1 ? prefix_len / kPage * kPage : 0;
+    std::vector<int32_t> lens(n_seqs), ids;
+    ids.reserve(total + (size_t)n_seqs * (prefix_len - share) + share);
+    const int32_t* next = prompt_ids;
+    for (int s = 0; s < n_seqs; ++s) {
+      const int from = s ? share : 0;
+      ids.insert(ids.end(), prefix_ids + from, prefix_ids + prefix_len);
+      ids.insert(ids.end(), next, next + prompt_lens[s]);
+      next += prompt_lens[s];
+      lens[s] = prefix_len - from + prompt_lens[s];
+    }
+    return e.prefill(n_seqs, lens.data(), ids.data(), gen_budget, share, first_tokens);
+  } catch (...) {
+    return fail(RT_ERR_INVALID, "unexpected exception in rt_prefill_prefix");
+  }
+}
+
+int rt_set_window(rt_model* m, int32_t window, int32_t sinks) {
+  if (!m || !m->e) return fail(RT_ERR_INVALID, "null model");
+  if (window < 0 || sinks < 0) return fail(RT_ERR_INVALID, "negative window or sinks");
+  if (window == 0 && sinks != 0) return fail(RT_ERR_INVALID, "sinks without a window");
+  EngineBase& e = *m->e;
+  e.window = window;
+  e.sinks = sinks;
+  e.prefilled = false;
+  e.drop_graph();
+  return RT_OK;
 }
 
 int rt_spec_round(rt_model* m, int32_t* tokens, int32_t* n_committed, int32_t* accept_len) {

@@ -396,9 +396,9 @@ void set_ints(int32_t* dst, int n, int v0, int v1, int v2, int v3, hipStream_t s
 }
 
 __global__ void first_tokens_kernel(int32_t* st_all, int seq0, const uint64_t* keys, const int32_t* sampled,
-                                    const int32_t* off, int budget, int32_t* first_out) {
+                                    const int32_t* off, int share, int budget, int32_t* first_out) {
   if (threadIdx.x != 0) return;
-  const int sq = seq0 + blockIdx.x, plen = off[sq + 1] - off[sq];
+  const int sq = seq0 + blockIdx.x, plen = off[sq + 1] - off[sq] + (sq > 0 ? share : 0);
   int32_t* st = st_all + sq * kStateFields;
   const int tok = sampled ? sampled[sq] : key_index(keys[blockIdx.x]);
   st[ST_SEQ_LEN] = plen;
@@ -413,9 +413,9 @@ __global__ void first_tokens_kernel(int32_t* st_all, int seq0, const uint64_t* k
   first_out[sq] = tok;
 }
 void first_tokens(int32_t* state, int seq0, int n, const uint64_t* keys, const int32_t* sampled, const int32_t* off,
-                  int budget, int32_t* first_out, hipStream_t s) {
+                  int share, int budget, int32_t* first_out, hipStream_t s) {
   if (n <= 0) return;
-  RT_LAUNCH(first_tokens_kernel, dim3(n), dim3(64), 0, s, state, seq0, keys, sampled, off, budget, first_out);
+  RT_LAUNCH(first_tokens_kernel, dim3(n), dim3(64), 0, s, state, seq0, keys, sampled, off, share, budget, first_out);
 }
 
 __global__ void gather_last_kernel(const float* __restrict__ x, int d, const int32_t* __restrict__ off, int seq0,

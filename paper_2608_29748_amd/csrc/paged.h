@@ -52,12 +52,15 @@ struct PagedPlan {
   int shared;                    // of the shared prefix (0: no pass of its own)
   // partial results per row: those of the prefix come first; one split of the rest joins them itself
   int parts() const { return shared + (splits > 1 ? splits : 0); }
+  int passes() const { return shared ? 2 : 1; }
+  int launches() const { return passes() + (splits > 1 ? 1 : 0); }      // the last one then the merge
 };
 PagedPlan paged_plan(const PagedAttnArgs& a, int elem_bytes);
-// Floats of part_o and part_ml.
+// Floats of part_o (returned) and part_ml.
 size_t paged_part_floats(const PagedAttnArgs& a, const PagedPlan& p, size_t* ml);
+// Launch i (0 .. p.launches() - 1, in order) of a call.
 template <typename T>
-hipError_t paged_attention(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s);
+hipError_t paged_launch(const PagedAttnArgs& a, const PagedPlan& p, int i, hipStream_t s);
 
 #ifdef __HIPCC__
 // Rows a .. a + n - 1 and key count of sequence s, as clamped.

@@ -144,7 +144,11 @@ static int attention(const rt_paged_kv* kv, const rt_attn_args* g, void* ws, siz
     a.part_o = (float*)ws;
     a.part_ml = (float*)((char*)ws + ml_off);
   }
-  return launched(esz == 2 ? paged_attention<bf16_t>(a, p, s) : paged_attention<float>(a, p, s), what);
+  for (int i = 0; i < p.launches(); ++i) {
+    const int e = launched(esz == 2 ? paged_launch<bf16_t>(a, p, i, s) : paged_launch<float>(a, p, i, s), what);
+    if (e) return e;
+  }
+  return RT_OK;
 }
 
 }  // namespace rt

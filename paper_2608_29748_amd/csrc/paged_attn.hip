@@ -866,48 +866,49 @@ size_t paged_part_floats(const PagedAttnArgs& a, const PagedPlan& p, size_t* ml)
 }
 
 template <typename T, int HD>
-static hipError_t attention_hd(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
+static hipError_t launch_pass(const PagedAttnArgs& a, const PagedPass& ps, hipStream_t s) {
   const PagedRows& r = a.r;
-  auto launch = [&](const PagedPass& ps) {
-    const bool t = tiled(a, ps.shared, sizeof(T));
-    const int nt = rows_nt(a, ps.shared, sizeof(T));
-    const long blocks = row_blocks(a, ps.shared, block_size(a, ps.shared, sizeof(T)));
-    const long grid = blocks * ps.splits * r.n_kv_heads;
-    if (grid <= 0) return hipSuccess;
-    if (grid > 0x7fffffffl) return hipErrorInvalidValue;
-    const dim3 gd((unsigned)grid);
-    if constexpr (sizeof(T) == 2) {
-      if (t) {
-        // a workgroup that has a compute unit to itself takes twice the stages
-        if (grid <= 256) RT_LAUNCH((paged_tile_kernel<HD, 4>), gd, dim3(256), 0, s, a, ps);
-        else RT_LAUNCH((paged_tile_kernel<HD, 2>), gd, dim3(256), 0, s, a, ps);
-        return hipGetLastError();
-      }
-    } else if constexpr (HD == 64) {
-      if (nt == 2) {
-        RT_LAUNCH((paged_rows_kernel<T, HD, 2, 4, false>), gd, dim3(256), 0, s, a, ps);
-        return hipGetLastError();
-      }
+  const bool t = tiled(a, ps.shared, sizeof(T));
+  const int nt = rows_nt(a, ps.shared, sizeof(T));
+  const long blocks = row_blocks(a, ps.shared, block_size(a, ps.shared, sizeof(T)));
+  const long grid = blocks * ps.splits * r.n_kv_heads;
+  if (grid <= 0) return hipSuccess;
+  if (grid > 0x7fffffffl) return hipErrorInvalidValue;
+  const dim3 gd((unsigned)grid);
+  if constexpr (sizeof(T) == 2) {
+    if (t) {
+      // a workgroup that has a compute unit to itself takes twice the stages
+      if (grid <= 256) RT_LAUNCH((paged_tile_kernel<HD, 4>), gd, dim3(256), 0, s, a, ps);
+      else RT_LAUNCH((paged_tile_kernel<HD, 2>), gd, dim3(256), 0, s, a, ps);
+      return hipGetLastError();
     }
-    if (streamed(a, ps.first, sizeof(T))) RT_LAUNCH((paged_rows_kernel<T, HD, 1, 4, true>), gd, dim3(256), 0, s, a, ps);
-    else RT_LAUNCH((paged_rows_kernel<T, HD, 1, 4, false>), gd, dim3(256), 0, s, a, ps);
-    return hipGetLastError();
-  };
-  hipError_t e = hipSuccess;
-  if (p.shared) e = launch(PagedPass{1, 0, p.shared, 0, 0});
-  const bool done = p.splits == 1;
-  if (e == hipSuccess) e = launch(PagedPass{0, p.shared ? a.prefix : 0, p.splits, done ? -1 : p.shared, done ? p.shared : 0});
-  if (e != hipSuccess || done) return e;
-  const long rows = (long)r.n_rows * r.n_q_heads;
+  } else if constexpr (HD == 64) {
+    if (nt == 2) {
+      RT_LAUNCH((paged_rows_kernel<T, HD, 2, 4, false>), gd, dim3(256), 0, s, a, ps);
+      return hipGetLastError();
+    }
+  }
+  if (streamed(a, ps.first, sizeof(T))) RT_LAUNCH((paged_rows_kernel<T, HD, 1, 4, true>), gd, dim3(256), 0, s, a, ps);
+  else RT_LAUNCH((paged_rows_kernel<T, HD, 1, 4, false>), gd, dim3(256), 0, s, a, ps);
+  return hipGetLastError();
+}
+template <typename T, int HD>
+static hipError_t launch_hd(const PagedAttnArgs& a, const PagedPlan& p, int i, hipStream_t s) {
+  if (i < p.passes()) {
+    if (p.shared && i == 0) return launch_pass<T, HD>(a, PagedPass{1, 0, p.shared, 0, 0}, s);
+    const bool done = p.splits == 1;
+    return launch_pass<T, HD>(a, PagedPass{0, p.shared ? a.prefix : 0, p.splits, done ? -1 : p.shared, done ? p.shared : 0}, s);
+  }
+  const long rows = (long)a.r.n_rows * a.r.n_q_heads;
   RT_LAUNCH((paged_merge_kernel<T, HD>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p.parts());
   return hipGetLastError();
 }
 template <typename T>
-hipError_t paged_attention(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
+hipError_t paged_launch(const PagedAttnArgs& a, const PagedPlan& p, int i, hipStream_t s) {
   if (a.r.n_rows <= 0 || a.r.n_seqs <= 0) return hipSuccess;
-  return a.r.head_dim == 128 ? attention_hd<T, 128>(a, p, s) : attention_hd<T, 64>(a, p, s);
+  return a.r.head_dim == 128 ? launch_hd<T, 128>(a, p, i, s) : launch_hd<T, 64>(a, p, i, s);
 }
-template hipError_t paged_attention<bf16_t>(const PagedAttnArgs&, const PagedPlan&, hipStream_t);
-template hipError_t paged_attention<float>(const PagedAttnArgs&, const PagedPlan&, hipStream_t);
+template hipError_t paged_launch<bf16_t>(const PagedAttnArgs&, const PagedPlan&, int, hipStream_t);
+template hipError_t paged_launch<float>(const PagedAttnArgs&, const PagedPlan&, int, hipStream_t);
 
 }  // namespace rt

@@ -241,10 +241,10 @@ int make_plan(const rt_config* c, Plan* p) {
   {
     // tokens and offsets; per (sequence, pass) segment at most rows / 64 + 1 attention blocks
     // and rows / 16 + 2 page items; per sequence once more the blocks that its last token's G
-    // rows meet; up to 3 ints of padding a pass
+    // rows meet; two ints a segment and one a pass; up to 3 ints of padding a pass
     const size_t tok = (size_t)q.bmax * q.T, pass = tok / q.PF + 2, seg = (size_t)q.bmax + pass;
     const size_t ends = (size_t)q.bmax * ((q.G + 62) / 64 + 1);
-    q.pf_tab_ints = tok + q.bmax + 1 + 8 * (tok * q.G / 64 + seg + ends) + 4 * (tok / 16 + 2 * seg) + 3 * pass;
+    q.pf_tab_ints = tok + q.bmax + 1 + 8 * (tok * q.G / 64 + seg + ends) + 4 * (tok / 16 + 2 * seg) + 2 * seg + 4 * pass;
     q.pf_tab = take(q.pf_tab_ints * 4);
   }
   q.ar_tok = take((size_t)q.bmax * kArMaxSteps * 4);

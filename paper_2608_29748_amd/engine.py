@@ -67,6 +67,16 @@ class RoundEngine:
         self.n_seqs = len(prompts)
         return first
 
+    def prefill_prefix(self, prefix: np.ndarray, prompts: Sequence[np.ndarray], gen_budget: int) -> np.ndarray:
+        """Prefill of prefix + prompt for every prompt, the prefix computed and kept once."""
+        first = B.rt_prefill_prefix(self.h, prefix, prompts, gen_budget)
+        self.n_seqs = len(prompts)
+        return first
+
+    def set_window(self, window: int, sinks: int = 0) -> None:
+        """Sliding window and sinks of the target's attention (0: full), from the next prefill on."""
+        B.rt_set_window(self.h, window, sinks)
+
     def spec_round(self):
         return B.rt_spec_round(self.h, self.n_seqs, self.cfg.block_size)
 
