@@ -58,7 +58,7 @@ __device__ __forceinline__ void norm_rotate(float (&x0)[8], float (&x1)[8], bool
 // Workgroups 0 .. n_kv-1: one page item (the rows of one sequence that fall into one page) and
 // one KV head each; the rest: queries, one wave per row and group of 64 / LPV heads.
 template <typename T, typename S, int HD>
-__global__ __launch_bounds__(4 * HD / 2) void append_kernel(AppendArgs a, int n_kv) {
+__global__ __launch_bounds__(2 * HD) void append_kernel(AppendArgs a, int n_kv) {
   constexpr int LPV = HD / 16;              // lanes per head vector
   constexpr int VPW = 64 / LPV;             // head vectors per wave
   constexpr int NT = 2 * HD;                // threads: 16 rows x LPV lanes for K, as many for V
@@ -73,12 +73,10 @@ __global__ __launch_bounds__(4 * HD / 2) void append_kernel(AppendArgs a, int n_
     for (int e = 0; e < 8; ++e) f.set(e, v[e]);
     f.store(p);
   };
-  // one head's vector at src (position pos, norm weights w or null), stored to dst where live
-  auto turn = [&](const S* src, long pos, const void* w, bool live, T* dst) {
+  // a head's vector x, with norm weights w (or null) and at position pos, to dst where live
+  auto turn = [&](const Frag<S> (&x)[2], long pos, const void* w, bool live, T* dst) {
     const bool rot = a.cos && u.rot;
-    float x0[8], x1[8], w0[8], w1[8], fc[8], fs[8];
-    load8(src + u.o0, x0);
-    load8(src + u.o1, x1);
+    float w0[8], w1[8], fc[8], fs[8];
     if (w) {
       load8((const T*)w + u.o0, w0);
       load8((const T*)w + u.o1, w1);
@@ -86,6 +84,12 @@ __global__ __launch_bounds__(4 * HD / 2) void append_kernel(AppendArgs a, int n_
     if (rot) {
       load8(a.cos + (size_t)pos * (a.rot_dim / 2) + 8 * c, fc);
       load8(a.sin + (size_t)pos * (a.rot_dim / 2) + 8 * c, fs);
+    }
+    float x0[8], x1[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x0[e] = x[0].get(e);
+      x1[e] = x[1].get(e);
     }
     norm_rotate<LPV>(x0, x1, w != nullptr, w0, w1, a.eps, rot, fc, fs);
     if (!live) return;
@@ -97,15 +101,18 @@ __global__ __launch_bounds__(4 * HD / 2) void append_kernel(AppendArgs a, int n_
     const int unit = ((int)blockIdx.x - n_kv) * (NT / 64) + (int)(threadIdx.x >> 6);
     const int row = unit / groups, h = unit % groups * VPW + lane / LPV;
     if (row >= r.n_rows) return;
+    const bool live = h < r.n_q_heads;
+    const int hh = live ? h : 0;
+    const S* src = (const S*)a.q + (size_t)row * a.ldq + (size_t)hh * HD;
+    Frag<S> x[2];                         // (under way while the row's position is found)
+    x[0].load(src + u.o0);
+    x[1].load(src + u.o1);
     const int s = row_seq(r, row);
     if (s >= r.n_seqs) return;
     const SeqRows sr = seq_rows(r, s);
     const long pos = (long)sr.keys - sr.n + (row - sr.a);
     if (row < sr.a || row >= sr.a + sr.n || pos < 0 || pos >= cap) return;
-    const bool live = h < r.n_q_heads;
-    const int hh = live ? h : 0;
-    turn((const S*)a.q + (size_t)row * a.ldq + (size_t)hh * HD, pos, a.q_norm, live,
-         (T*)a.q_out + (size_t)row * a.ldqo + (size_t)hh * HD);
+    turn(x, pos, a.q_norm, live, (T*)a.q_out + (size_t)row * a.ldqo + (size_t)hh * HD);
     return;
   }
   const int kvh = (int)blockIdx.x % r.n_kv_heads, item = (int)blockIdx.x / r.n_kv_heads;
@@ -128,8 +135,11 @@ __global__ __launch_bounds__(4 * HD / 2) void append_kernel(AppendArgs a, int n_
   if (threadIdx.x < NT / 2) {                                     // K: slot t, LPV lanes
     const int t = threadIdx.x / LPV;
     if (t < lo || t >= hi) return;        // (whole LPV groups leave together)
-    turn((const S*)a.ks + (size_t)(row0 + t) * a.ldk + (size_t)kvh * HD, pg * kPage + t, a.k_norm, true,
-         (T*)r.k + base + (size_t)t * HD);
+    const S* src = (const S*)a.ks + (size_t)(row0 + t) * a.ldk + (size_t)kvh * HD;
+    Frag<S> x[2];
+    x[0].load(src + u.o0);
+    x[1].load(src + u.o1);
+    turn(x, pg * kPage + t, a.k_norm, true, (T*)r.k + base + (size_t)t * HD);
   } else {                                                        // V: element d of every slot
     const int d = threadIdx.x - NT / 2;
     T* dst = (T*)r.v + base + (size_t)d * kPage;
