@@ -467,20 +467,18 @@ struct Engine : EngineBase {
     if (c.blocks && c.n_blocks == 0) return RT_OK;      // (the last layer of prompts that do not end in this pass)
     for (int i = 0; i < pl.launches(); ++i) {
       double bytes = 0, flops = 0;
-      const bool pass = i < pl.passes(), pre = pl.shared && i == 0;
       if (instrumented()) {   // (prompt passes are not instrumented)
         const double E = sizeof(T), rows = (double)c.n_seqs * c.rows_per_seq;
-        double keys = pre ? a.prefix : 0;
-        for (int s = 0; s < c.n_seqs && !pre; ++s) {
-          const double n = c.prof_ctx[s] + c.rows_per_seq - (pl.shared ? a.prefix : 0);
+        double keys = 0, shared_keys = pl.shared ? a.prefix : 0;
+        for (int s = 0; s < c.n_seqs; ++s) {
+          const double n = c.prof_ctx[s] + c.rows_per_seq - shared_keys;
           keys += a.window > 0 ? fmin(n, (double)a.window + a.sinks + c.rows_per_seq - 1) : n;
         }
-        const double part = rows * q.Hq * (q.hd + 2) * 4.0;
-        bytes = pass ? keys * 2.0 * q.Hkv * q.hd * E + rows * q.qN * E : part * pl.parts();
-        if (pass) bytes += pre ? part * pl.shared : pl.splits > 1 ? part * pl.splits : part * pl.shared + rows * q.qN * E;
-        flops = pass ? 4.0 * keys * (pre ? rows : c.rows_per_seq) * q.Hq * q.hd : 0;
+        const double parts = rows * q.Hq * (q.hd + 2) * 4.0 * pl.parts(), out = rows * q.qN * E;
+        bytes = i == 0 ? (keys + shared_keys) * 2.0 * q.Hkv * q.hd * E + out + (pl.parts() ? parts : out) : parts + out;
+        flops = i == 0 ? 4.0 * (keys * c.rows_per_seq + shared_keys * rows) * q.Hq * q.hd : 0;
       }
-      prof_begin(pass ? RT_K_ATTENTION : RT_K_ATTN_MERGE, bytes, flops);
+      prof_begin(i == 0 ? RT_K_ATTENTION : RT_K_ATTN_MERGE, bytes, flops);
       HIPCHK(paged_launch<T>(a, pl, i, stream));
       prof_end();
     }

@@ -50,10 +50,9 @@ struct PagedAttnArgs {
 struct PagedPlan {
   int splits;                    // of the sequences' own keys
   int shared;                    // of the shared prefix (0: no pass of its own)
-  // partial results per row: those of the prefix come first; one split of the rest joins them itself
-  int parts() const { return shared + (splits > 1 ? splits : 0); }
-  int passes() const { return shared ? 2 : 1; }
-  int launches() const { return passes() + (splits > 1 ? 1 : 0); }      // the last one then the merge
+  // partial results per row, those of the prefix first (0: rows are finished in one go)
+  int parts() const { return shared || splits > 1 ? shared + splits : 0; }
+  int launches() const { return parts() ? 2 : 1; }      // the passes, the merge
 };
 PagedPlan paged_plan(const PagedAttnArgs& a, int elem_bytes);
 // Floats of part_o (returned) and part_ml.

@@ -10,8 +10,8 @@
 // Visible keys of a row: [lo, hi) and the sinks [0, snk), snk <= lo:
 //   window      hi = p + 1, lo = p - window + 1, snk = sinks
 //   prefix      where it pays, keys [0, prefix) in a pass over the rows of all sequences, whose
-//               tiles so fill with rows that read the same pages, and then [prefix, p] sequence
-//               by sequence, joined with what the first pass left.
+//               tiles so fill with rows that read the same pages, and beside it [prefix, p]
+//               sequence by sequence; a merge joins them.
 #include "paged.h"
 
 namespace rt {
@@ -22,14 +22,14 @@ constexpr int kStep = 32;                  // keys per step of a wave: two pages
 constexpr int kMaxParts = 32;              // key splits of a pass
 constexpr float kMrefInit = -1.0e30f;      // running maximum before any visible key (log2 units)
 
-// One launch of a call: over the shared prefix, or over the sequences' own keys (all of them where
-// no pass is made over the prefix).
+// A pass of a call: over the shared prefix, or over the sequences' own keys (all of them where no
+// pass is made over the prefix).  Both go out in one launch, the prefix's workgroups first.
 struct PagedPass {
   int shared;       // 1: the rows of all sequences over the prefix
   int first;        // key from which on the sequences' own pass works (0, or the prefix)
   int splits;
-  int z0;           // partial results go to parts z0 .. z0 + splits - 1; -1: rows are finished here,
-  int join;         // together with parts 0 .. join - 1
+  int z0;           // partial results go to parts z0 .. z0 + splits - 1; -1: rows are finished here
+  int groups;       // workgroups
 };
 
 struct RowRange { int lo, hi, snk; };
@@ -132,19 +132,24 @@ __device__ __forceinline__ int wave_max(int v) { return __builtin_amdgcn_readfir
 // that only this workgroup reads come by non-temporal loads (NTL).  64 steps over 4100 keys, 40 heads
 // (1.08 GB): 165 us (6.5 TB/s); with plain loads 185, with three waves per SIMD 197, with a second set
 // of registers for the next step's keys 208.
+template <int HD, int NT, int NW>
+struct RowsLds {
+  float o[NW][16 * NT][HD + 4];                            // results of the waves
+  float ml[NW][16 * NT][2];
+  float p[NW][kStep][16];                                  // one tile's weights (non-finite V only)
+};
 template <typename T, int HD, int NT, int NW, bool NTL>
-__global__ __launch_bounds__(64 * NW, 2) void paged_rows_kernel(PagedAttnArgs a, PagedPass ps) {
+__device__ __forceinline__ void rows_body(const PagedAttnArgs& a, const PagedPass& ps, int group, RowsLds<HD, NT, NW>& lds) {
   constexpr int NHT = HD / 16, NKS = HD / 32;
   constexpr int RB = 16 * NT;
-  constexpr int OP = HD + 4;                               // fp32 pitch of a merged row
-  __shared__ __attribute__((aligned(16))) float sO[NW][RB][OP];
-  __shared__ float sML[NW][RB][2];
-  __shared__ float sP[NW][kStep][16];                      // one tile's weights (non-finite V only)
+  auto& sO = lds.o;
+  auto& sML = lds.ml;
+  auto& sP = lds.p;
   const PagedRows& r = a.r;
   const int lane = threadIdx.x & 63, g4 = lane >> 4, c16 = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = blockIdx.x % r.n_kv_heads, split = blockIdx.x / r.n_kv_heads % ps.splits;
-  const int blk = blockIdx.x / (r.n_kv_heads * ps.splits);
+  const int kvh = group % r.n_kv_heads, split = group / r.n_kv_heads % ps.splits;
+  const int blk = group / (r.n_kv_heads * ps.splits);
   const int G = r.n_q_heads / r.n_kv_heads;
   int s, rb;
   SeqRows sr;
@@ -342,7 +347,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_rows_kernel(PagedAttnArgs a,
   __syncthreads();
   const int items = min(RB, nrows - row0) * RUNS;
   const size_t zst = (size_t)r.n_rows * r.n_q_heads;
-  const int it = threadIdx.x % items, grp = threadIdx.x / items;      // (groups: the prefix parts, below)
+  if ((int)threadIdx.x >= items) return;
+  const int it = threadIdx.x;
   const int rl = it / RUNS, d = it % RUNS * 8, rr = row0 + rl;
   const int tok = sr.a + rr / G, h = kvh * G + rr % G;
   const size_t rh = (size_t)tok * r.n_q_heads + h;
@@ -356,48 +362,6 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_rows_kernel(PagedAttnArgs a,
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += f * sO[u][rl][d + e];
   }
-  if (ps.join) {
-    // with the prefix: its parts' maxima and sums through LDS, its elements shared out over as many
-    // threads per item as there are
-    const int zs = ps.join, groups = 64 * NW / items;
-    float2* const pml = reinterpret_cast<float2*>(&sP[0][0][0]);
-    static_assert(sizeof(sP) >= RB * kMaxParts * sizeof(float2), "maxima and sums of the parts");
-    for (int i = threadIdx.x; i < items / RUNS * zs; i += 64 * NW) {
-      const int row = row0 + i / zs, tk = sr.a + row / G, hd = kvh * G + row % G;
-      pml[i] = *reinterpret_cast<const float2*>(a.part_ml + ((i % zs) * zst + (size_t)tk * r.n_q_heads + hd) * 2);
-    }
-    __syncthreads();
-    float m = M;
-    for (int z = 0; z < zs; ++z) m = fmaxf(m, pml[rl * zs + z].x);
-    const float f0 = __builtin_amdgcn_exp2f(M - m);
-    L *= f0;
-    for (int z = 0; z < zs; ++z) L += __builtin_amdgcn_exp2f(pml[rl * zs + z].x - m) * pml[rl * zs + z].y;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = grp == 0 ? v[e] * f0 : 0.f;
-    if (grp < groups) {
-      const float* op = a.part_o + rh * HD + d;
-#pragma unroll 4
-      for (int z = grp; z < zs; z += groups) {
-        const float f = __builtin_amdgcn_exp2f(pml[rl * zs + z].x - m);
-        const float4 a0 = *reinterpret_cast<const float4*>(op + z * zst * HD);
-        const float4 a1 = *reinterpret_cast<const float4*>(op + z * zst * HD + 4);
-        v[0] += f * a0.x; v[1] += f * a0.y; v[2] += f * a0.z; v[3] += f * a0.w;
-        v[4] += f * a1.x; v[5] += f * a1.y; v[6] += f * a1.z; v[7] += f * a1.w;
-      }
-    }
-    if (groups > 1) {
-      float* const sv = &sO[0][0][0];                  // [group][item][8] (every wave is past its reads)
-      if (grp > 0 && grp < groups)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sv[(grp * items + it) * 8 + e] = v[e];
-      __syncthreads();
-      if (grp == 0)
-        for (int u = 1; u < groups; ++u)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] += sv[(u * items + it) * 8 + e];
-    }
-  }
-  if (grp > 0) return;
   if (ps.z0 >= 0) {
     const size_t row = (ps.z0 + split) * zst + rh;
     float* op = a.part_o + row * HD + d;
@@ -443,19 +407,24 @@ __device__ __forceinline__ void copy_page(const char* src, char* dst, const int*
 }
 
 template <int HD, int NST>
-__global__ __launch_bounds__(256, NST > 2 ? 1 : HD == 64 ? 3 : 2) void paged_tile_kernel(PagedAttnArgs a, PagedPass ps) {
+struct TileLds {
+  char stage[NST * 2 * (kChunkT / kPage) * kPage * HD * 2];
+};
+template <int HD, int NST>
+__device__ __forceinline__ void tile_body(const PagedAttnArgs& a, const PagedPass& ps, int group, TileLds<HD, NST>& lds) {
   constexpr int ROWB = HD * 2, NP = ROWB / 16, PGB = kPage * ROWB, NLD = PGB / 1024;
   constexpr int PAGES = kChunkT / kPage, STG = 2 * PAGES * PGB;
   constexpr int NKS = HD / 16, NDT = HD / 32;
   constexpr int OPB = ROWB + 16;                       // pitch of a finished row in LDS
   static_assert(2 * STG >= kTileRows * OPB, "finished rows fit the stages");
   static_assert(NST == 2 || NST == 4, "stage offsets wrap by a mask");
-  __shared__ __attribute__((aligned(1024))) char smem[NST * STG];
+  static_assert(sizeof(lds.stage) == NST * STG, "stages");
+  char* const smem = lds.stage;
   const PagedRows& r = a.r;
   const int lane = threadIdx.x & 63, g = lane >> 5, c32 = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = blockIdx.x % r.n_kv_heads, split = blockIdx.x / r.n_kv_heads % ps.splits;
-  const int blk = blockIdx.x / (r.n_kv_heads * ps.splits);
+  const int kvh = group % r.n_kv_heads, split = group / r.n_kv_heads % ps.splits;
+  const int blk = group / (r.n_kv_heads * ps.splits);
   const int G = r.n_q_heads / r.n_kv_heads;
   int s, rb;
   SeqRows sr;
@@ -711,30 +680,6 @@ __global__ __launch_bounds__(256, NST > 2 ? 1 : HD == 64 ? 3 : 2) void paged_til
     }
     return;
   }
-  if (ps.join) {       // with the parts of the prefix
-#pragma unroll 2
-    for (int z = 0; z < ps.join; ++z) {
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (z * zst + rh) * 2);
-      const float* op = a.part_o + (z * zst + rh) * HD + 4 * g;
-      float4 p[NDT][4];
-#pragma unroll
-      for (int d = 0; d < NDT; ++d)
-#pragma unroll
-        for (int b = 0; b < 4; ++b) p[d][b] = *reinterpret_cast<const float4*>(op + d * 32 + 8 * b);
-      const float M = fmaxf(mref, ml.x), f0 = __builtin_amdgcn_exp2f(mref - M), f = __builtin_amdgcn_exp2f(ml.x - M);
-      mref = M;
-      lsum = f0 * lsum + f * ml.y;
-#pragma unroll
-      for (int d = 0; d < NDT; ++d)
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          o[d][4 * b] = f0 * o[d][4 * b] + f * p[d][b].x;
-          o[d][4 * b + 1] = f0 * o[d][4 * b + 1] + f * p[d][b].y;
-          o[d][4 * b + 2] = f0 * o[d][4 * b + 2] + f * p[d][b].z;
-          o[d][4 * b + 3] = f0 * o[d][4 * b + 3] + f * p[d][b].w;
-        }
-    }
-  }
   // finished rows through LDS, so that they leave 16 bytes a lane along the row
   const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
   lds_barrier();
@@ -762,44 +707,80 @@ __global__ __launch_bounds__(256, NST > 2 ? 1 : HD == 64 ? 3 : 2) void paged_til
   }
 }
 
-// Joins the z partial results of every (row, head): one wave each, HD / 64 elements a lane.
+// The launches: workgroups below p0.groups work on the first pass, the others on the second.
+template <typename T, int HD, int NT, int NW, bool NTL>
+__global__ __launch_bounds__(64 * NW, 2) void paged_rows_kernel(PagedAttnArgs a, PagedPass p0, PagedPass p1) {
+  __shared__ __attribute__((aligned(16))) RowsLds<HD, NT, NW> lds;
+  const bool first = (int)blockIdx.x < p0.groups;
+  rows_body<T, HD, NT, NW, NTL>(a, first ? p0 : p1, blockIdx.x - (first ? 0 : p0.groups), lds);
+}
+template <int HD, int NST>
+__global__ __launch_bounds__(256, NST > 2 ? 1 : HD == 64 ? 3 : 2) void paged_tile_kernel(PagedAttnArgs a, PagedPass p0,
+                                                                                       PagedPass p1) {
+  __shared__ __attribute__((aligned(1024))) TileLds<HD, NST> lds;
+  const bool first = (int)blockIdx.x < p0.groups;
+  tile_body<HD, NST>(a, first ? p0 : p1, blockIdx.x - (first ? 0 : p0.groups), lds);
+}
+// The prefix in tiles, the sequences' own keys by rows: the first is bound by arithmetic, the second
+// by memory, and a compute unit runs one of each.
+template <int HD, bool NTL>
+__global__ __launch_bounds__(256, 2) void paged_both_kernel(PagedAttnArgs a, PagedPass p0, PagedPass p1) {
+  union Lds {
+    TileLds<HD, 2> t;
+    RowsLds<HD, 1, 4> r;
+  };
+  __shared__ __attribute__((aligned(1024))) char lds[sizeof(Lds)];
+  if ((int)blockIdx.x < p0.groups) tile_body<HD, 2>(a, p0, blockIdx.x, reinterpret_cast<Lds*>(lds)->t);
+  else rows_body<bf16_t, HD, 1, 4, NTL>(a, p1, blockIdx.x - p0.groups, reinterpret_cast<Lds*>(lds)->r);
+}
+
+// Joins the zs partial results of every (row, head), one wave each: sums and weights over the
+// lanes, a part each, then the parts' elements, four a lane, 256 / HD parts at a time.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a, int zs) {
-  constexpr int E = HD / 64;
+  constexpr int LPR = HD / 4, ZG = 64 / LPR;              // lanes of a part, parts at a time
   const PagedRows& r = a.r;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, zg = lane / LPR, d = lane % LPR * 4;
   const long rh = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (rh >= (long)r.n_rows * r.n_q_heads) return;
   const int tok = (int)(rh / r.n_q_heads), h = (int)(rh % r.n_q_heads);
+  const size_t zst = (size_t)r.n_rows * r.n_q_heads;
+  float2 ml = make_float2(kMrefInit, 0.f);
+  if (lane < zs) ml = *reinterpret_cast<const float2*>(a.part_ml + (lane * zst + rh) * 2);
   const int s = row_seq(r, tok);
   if (s >= r.n_seqs) return;               // a row behind the last sequence: left as it was
   const SeqRows sr = seq_rows(r, s);
   if (tok < sr.a || tok >= sr.a + sr.n) return;
-  const size_t zst = (size_t)r.n_rows * r.n_q_heads;
-  float m = kMrefInit, l = 0.f;
-  if (lane < zs) {
-    m = a.part_ml[(lane * zst + rh) * 2];
-    l = a.part_ml[(lane * zst + rh) * 2 + 1];
-  }
-  const float M = warp_max(m);
-  const float f = lane < zs ? __builtin_amdgcn_exp2f(m - M) : 0.f;
-  const float L = warp_sum(f * l);
-  float v[E];
+  const float M = warp_max(ml.x);
+  const float f = lane < zs ? __builtin_amdgcn_exp2f(ml.x - M) : 0.f;
+  const float L = warp_sum(f * ml.y);
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  const float* op = a.part_o + rh * HD + d;
+  for (int z0 = 0; z0 < zs; z0 += 4 * ZG) {
+    float4 p[4];
 #pragma unroll
-  for (int e = 0; e < E; ++e) v[e] = 0.f;
-  for (int z = 0; z < zs; ++z) {
-    const float fz = __shfl(f, z, 64);
-    const float* op = a.part_o + (z * zst + rh) * HD + lane * E;
+    for (int u = 0; u < 4; ++u) {
+      const int z = z0 + u * ZG + zg;
+      p[u] = z < zs ? *reinterpret_cast<const float4*>(op + z * zst * HD) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] += fz * op[e];
+    for (int u = 0; u < 4; ++u) {
+      const int z = z0 + u * ZG + zg;
+      const float fz = __shfl(f, z & 63, 64);
+      if (z >= zs) continue;
+      v[0] += fz * p[u].x; v[1] += fz * p[u].y; v[2] += fz * p[u].z; v[3] += fz * p[u].w;
+    }
   }
+#pragma unroll
+  for (int o = LPR; o < 64; o <<= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += __shfl_xor(v[e], o, 64);
+  if (zg) return;
   const float inv = L == 0.f ? 0.f : 1.f / L;
+  const int col = h * HD + d;
+  T* out = (T*)a.out + (a.packed ? pa_index(tok, col, (size_t)a.ldo) : (size_t)tok * a.ldo + col);
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int col = h * HD + lane * E + e;
-    const size_t at = a.packed ? pa_index(tok, col, (size_t)a.ldo) : (size_t)tok * a.ldo + col;
-    ((T*)a.out)[at] = Elem<T>::from_f32(L == 0.f ? 0.f : v[e] * inv);
-  }
+  for (int e = 0; e < 4; ++e) out[e] = Elem<T>::from_f32(L == 0.f ? 0.f : v[e] * inv);
 }
 
 // ------------------------------------------------------------------ host
@@ -814,17 +795,19 @@ static long row_blocks(const PagedAttnArgs& a, bool shared, int rb) {
 static long rows_of(const PagedAttnArgs& a, bool shared) {
   return (long)(shared ? a.r.n_rows : a.max_rows) * (a.r.n_q_heads / a.r.n_kv_heads);
 }
-// Query tiles of a wave of the rows kernel: two where fp32 rows fill them and the registers hold them,
-// so that a page is read half as often.
-static int rows_nt(const PagedAttnArgs& a, bool shared, int elem_bytes) {
-  return elem_bytes == 4 && a.r.head_dim == 64 && rows_of(a, shared) > 16 ? 2 : 1;
+// Query tiles of a wave of the rows kernel: two where fp32 rows make many blocks and the registers
+// hold them, so that a page is read half as often.
+static int rows_nt(const PagedAttnArgs& a, int elem_bytes) {
+  const PagedRows& r = a.r;
+  return elem_bytes == 4 && r.head_dim == 64 && rows_of(a, false) > 16 &&
+                 row_blocks(a, false, 16) * r.n_kv_heads > 2048 ? 2 : 1;
 }
 // bf16 passes of more than 16 (token, head) rows a block take the tile kernel.
 static bool tiled(const PagedAttnArgs& a, bool shared, int elem_bytes) {
   return elem_bytes == 2 && rows_of(a, shared) > 16;
 }
 static int block_size(const PagedAttnArgs& a, bool shared, int elem_bytes) {
-  return tiled(a, shared, elem_bytes) ? kTileRows : 16 * rows_nt(a, shared, elem_bytes);
+  return tiled(a, shared, elem_bytes) ? kTileRows : 16 * rows_nt(a, elem_bytes);
 }
 
 // Keys of a sequence that a pass from key `first` on reads, as far as the host knows.
@@ -866,41 +849,43 @@ size_t paged_part_floats(const PagedAttnArgs& a, const PagedPlan& p, size_t* ml)
 }
 
 template <typename T, int HD>
-static hipError_t launch_pass(const PagedAttnArgs& a, const PagedPass& ps, hipStream_t s) {
+static hipError_t launch_hd(const PagedAttnArgs& a, const PagedPlan& p, int i, hipStream_t s) {
   const PagedRows& r = a.r;
-  const bool t = tiled(a, ps.shared, sizeof(T));
-  const int nt = rows_nt(a, ps.shared, sizeof(T));
-  const long blocks = row_blocks(a, ps.shared, block_size(a, ps.shared, sizeof(T)));
-  const long grid = blocks * ps.splits * r.n_kv_heads;
-  if (grid <= 0) return hipSuccess;
-  if (grid > 0x7fffffffl) return hipErrorInvalidValue;
-  const dim3 gd((unsigned)grid);
+  if (i > 0) {
+    const long rows = (long)r.n_rows * r.n_q_heads;
+    RT_LAUNCH((paged_merge_kernel<T, HD>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p.parts());
+    return hipGetLastError();
+  }
+  const long E = sizeof(T);
+  const bool t0 = p.shared && tiled(a, true, E), t1 = tiled(a, false, E);
+  const long g0 = p.shared ? row_blocks(a, true, block_size(a, true, E)) * p.shared * r.n_kv_heads : 0;
+  const long g1 = row_blocks(a, false, block_size(a, false, E)) * p.splits * r.n_kv_heads;
+  if (g0 + g1 <= 0) return hipSuccess;
+  if (g0 + g1 > 0x7fffffffl) return hipErrorInvalidValue;
+  const PagedPass p0{1, 0, p.shared, 0, (int)g0};
+  const PagedPass p1{0, p.shared ? a.prefix : 0, p.splits, p.parts() ? p.shared : -1, (int)g1};
+  const dim3 gd((unsigned)(g0 + g1));
+  const bool ntl = streamed(a, p1.first, E);
   if constexpr (sizeof(T) == 2) {
-    if (t) {
+    if (t1) {          // (rows that fill tiles of their own fill them over the prefix too)
       // a workgroup that has a compute unit to itself takes twice the stages
-      if (grid <= 256) RT_LAUNCH((paged_tile_kernel<HD, 4>), gd, dim3(256), 0, s, a, ps);
-      else RT_LAUNCH((paged_tile_kernel<HD, 2>), gd, dim3(256), 0, s, a, ps);
+      if (g0 + g1 <= 256) RT_LAUNCH((paged_tile_kernel<HD, 4>), gd, dim3(256), 0, s, a, p0, p1);
+      else RT_LAUNCH((paged_tile_kernel<HD, 2>), gd, dim3(256), 0, s, a, p0, p1);
+      return hipGetLastError();
+    }
+    if (t0) {
+      if (ntl) RT_LAUNCH((paged_both_kernel<HD, true>), gd, dim3(256), 0, s, a, p0, p1);
+      else RT_LAUNCH((paged_both_kernel<HD, false>), gd, dim3(256), 0, s, a, p0, p1);
       return hipGetLastError();
     }
   } else if constexpr (HD == 64) {
-    if (nt == 2) {
-      RT_LAUNCH((paged_rows_kernel<T, HD, 2, 4, false>), gd, dim3(256), 0, s, a, ps);
+    if (rows_nt(a, E) == 2) {
+      RT_LAUNCH((paged_rows_kernel<T, HD, 2, 4, false>), gd, dim3(256), 0, s, a, p0, p1);
       return hipGetLastError();
     }
   }
-  if (streamed(a, ps.first, sizeof(T))) RT_LAUNCH((paged_rows_kernel<T, HD, 1, 4, true>), gd, dim3(256), 0, s, a, ps);
-  else RT_LAUNCH((paged_rows_kernel<T, HD, 1, 4, false>), gd, dim3(256), 0, s, a, ps);
-  return hipGetLastError();
-}
-template <typename T, int HD>
-static hipError_t launch_hd(const PagedAttnArgs& a, const PagedPlan& p, int i, hipStream_t s) {
-  if (i < p.passes()) {
-    if (p.shared && i == 0) return launch_pass<T, HD>(a, PagedPass{1, 0, p.shared, 0, 0}, s);
-    const bool done = p.splits == 1;
-    return launch_pass<T, HD>(a, PagedPass{0, p.shared ? a.prefix : 0, p.splits, done ? -1 : p.shared, done ? p.shared : 0}, s);
-  }
-  const long rows = (long)a.r.n_rows * a.r.n_q_heads;
-  RT_LAUNCH((paged_merge_kernel<T, HD>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p.parts());
+  if (ntl) RT_LAUNCH((paged_rows_kernel<T, HD, 1, 4, true>), gd, dim3(256), 0, s, a, p0, p1);
+  else RT_LAUNCH((paged_rows_kernel<T, HD, 1, 4, false>), gd, dim3(256), 0, s, a, p0, p1);
   return hipGetLastError();
 }
 template <typename T>
