@@ -816,24 +816,35 @@ static long keys_of(const PagedAttnArgs& a, long first) {
   return a.window > 0 && keys > seen ? seen : keys < 0 ? 0 : keys;
 }
 // Whether the rows kernel's pages come by non-temporal loads: where each is read by one workgroup
-// and all of them are more than the 256 MB memory-side cache holds (1.08 GB: 165 us against 185;
-// 134 MB that lay in that cache: 41 us against 30).
+// and all of them may be more than twice the 256 MB memory-side cache (64 steps over 4100 keys, 1.08
+// GB: 165 us against 185; 64 steps over up to 1024 keys of their own beside a prefix, at most 268
+// MB: 58.2 us against 54.4 with plain loads).
 static bool streamed(const PagedAttnArgs& a, long first, int elem_bytes) {
   const PagedRows& r = a.r;
-  return a.prefix <= first && 2.0 * r.n_seqs * keys_of(a, first) * r.n_kv_heads * r.head_dim * elem_bytes > 256e6;
+  return a.prefix <= first && 2.0 * r.n_seqs * keys_of(a, first) * r.n_kv_heads * r.head_dim * elem_bytes > 512e6;
 }
 
 PagedPlan paged_plan(const PagedAttnArgs& a, int elem_bytes) {
   const PagedRows& r = a.r;
   PagedPlan p{1, 0};
   // A pass over the shared prefix of its own pays where the sequences' rows do not fill tiles by
-  // themselves and reading the prefix once for each would move much more than reading it once.
+  // themselves and reading the prefix once for each would move over 230 MB more than reading it once.
+  // In one pass against two, 8 KV heads of 128: single tokens of 8 sequences behind 4096 keys (117 MB)
+  // 18.7 us, 26.6; 8 behind 8192 (235 MB) 28.2, 27.0; 64 behind 1024 (264 MB) 32.8, 32.4; 16 behind 8192
+  // (503 MB) 47.4, 28.6.  Blocks of 16 tokens: 16 behind 2048 (126 MB) 29.3, 33.4; 8 behind 8192 34.9,
+  // 34.0; 32 behind 2048 (260 MB) 39.9, 35.1; 16 behind 8192 55.8, 36.7.
   const double pre = 2.0 * a.prefix * r.n_kv_heads * r.head_dim * elem_bytes;
-  const bool apart = a.prefix > 0 && rows_of(a, false) < kTileRows && (r.n_seqs - 1.33) * pre > 40e6;
+  const bool apart = a.prefix > 0 && rows_of(a, false) < kTileRows && (r.n_seqs - 1) * pre > 230e6;
   auto pick = [&](bool shared, long keys) {
     const long units = row_blocks(a, shared, block_size(a, shared, elem_bytes)) * r.n_kv_heads;
     long s = 512 / units;
-    const long most = keys / (tiled(a, shared, elem_bytes) ? 8 * kChunkT : 8 * kStep);
+    // keys of a split: enough for its start and its part to be small beside them.  Over a prefix of 8192
+    // keys, whose parts are written and read for every row of the batch (64 steps, 32 heads): splits
+    // of 256, 512, 1024 and 2048 keys 63.6, 54.4, 48.1 and 61.3 us.
+    // Up to 640 keys of rows go without a merge (577 keys, four sequences: 10.6 us in one launch, 11.5 in
+    // two; 1028 keys, one sequence: 15.3 and 11.6).
+    long most = keys / (!tiled(a, shared, elem_bytes) ? 8 * kStep : shared ? 16 * kChunkT : 8 * kChunkT);
+    if (!shared && !tiled(a, shared, elem_bytes) && keys <= 640) most = 1;
     if (s > most) s = most;
     return (int)(s < 1 ? 1 : s > kMaxParts ? kMaxParts : s);
   };

@@ -378,9 +378,9 @@ def test_two_streams_at_once(ops):
 
 
 @pytest.mark.parametrize("heads,dtype,seqs,prefix,rows", [
-    ((8, 8, 128), BF, 40, 512, [1]), ((40, 8, 128), BF, 33, 528, [1]), ((16, 8, 64), BF, 60, 1024, [3]),
-    ((16, 8, 128), BF, 24, 1040, [0, 1, 5, 16]), ((4, 4, 64), F32, 64, 512, [1]), ((8, 4, 128), F32, 30, 800, [2]),
-    ((6, 2, 64), F32, 64, 1040, [0, 1, 2, 9])], ids=repr)
+    ((8, 8, 128), BF, 40, 1600, [1]), ((40, 8, 128), BF, 33, 2000, [1]), ((16, 8, 64), BF, 60, 2096, [3]),
+    ((16, 8, 128), BF, 24, 2608, [0, 1, 5, 16]), ((4, 4, 64), F32, 64, 2000, [1]), ((8, 4, 128), F32, 30, 2080, [2]),
+    ((6, 2, 64), F32, 64, 3856, [0, 1, 2, 9])], ids=repr)
 def test_prefix_in_a_pass_of_its_own(ops, heads, dtype, seqs, prefix, rows):
     """Batches that make the prefix pass worth its launch (the workspace holds its parts)."""
     rows = [rows[i % len(rows)] for i in range(seqs)]
@@ -394,10 +394,11 @@ def test_prefix_in_a_pass_of_its_own(ops, heads, dtype, seqs, prefix, rows):
     assert (out[-2:] == 7).all()
 
 
-@pytest.mark.parametrize("heads,dtype,rows", [((8, 8, 128), BF, 1), ((16, 8, 64), BF, 16), ((4, 4, 64), F32, 2)], ids=repr)
-def test_prefix_pass_and_splits_of_the_rest(ops, heads, dtype, rows):
+@pytest.mark.parametrize("heads,dtype,rows,prefix", [((8, 8, 128), BF, 1, 4608), ((16, 8, 64), BF, 16, 9216),
+                                                     ((4, 4, 64), F32, 2, 9216)], ids=repr)
+def test_prefix_pass_and_splits_of_the_rest(ops, heads, dtype, rows, prefix):
     """Long sequences of their own behind a long prefix: parts of both meet in the merge."""
-    prefix, S = 2048, 14
+    S = 14
     c = Case([rows] * S, [prefix + rows + 300 * i for i in range(S)], heads, dtype, seed=1, ragged=False, shared=prefix)
     check(attend(ops, c, prefix=prefix, max_kv=max(c.keys)), *ref_attention(c))
 
