@@ -274,9 +274,10 @@ typedef struct rt_append_args {
 int rt_kv_append(const rt_paged_kv* kv, const rt_append_args* args, void* hip_stream);
 
 /* Grouped-query attention of the rows over the cache: query head h reads KV head
- * h / (n_q_heads / n_kv_heads).  Sums and softmax statistics are fp32; rows that see no key give
- * zeros.  What lies in places of the cache that a row does not see, infinities and NaN included,
- * does not reach its output.
+ * h / (n_q_heads / n_kv_heads).  Sums and softmax statistics are fp32, for scaled scores within
+ * 2^24 of zero (beyond, neighbouring fp32 numbers are more than one apart); rows that see no key, or
+ * none with a score above minus infinity, give zeros.  What lies in places of the cache that a row does not
+ * see, infinities and NaN included, does not reach its output; what it sees may make it infinite or NaN.
  *
  * rt_window_attention: the row at position p sees the keys j <= p with j > p - window (the
  * window, its own position included) or j < sinks (the first tokens, which stay visible).

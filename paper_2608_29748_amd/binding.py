@@ -222,6 +222,8 @@ def rt_prefill_prefix(h: int, prefix: np.ndarray, prompts: Sequence[np.ndarray],
 
 
 def rt_set_window(h: int, window: int, sinks: int = 0) -> None:
+    if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):
+        raise RetraceError(RT_ERR_INVALID, "window and sinks must be in [0, 2^31)")
     _check(_lib.rt_set_window(C.c_void_p(h), window, sinks))
 
 

@@ -61,6 +61,8 @@ size_t paged_part_floats(const PagedAttnArgs& a, const PagedPlan& p, size_t* ml)
 template <typename T>
 hipError_t paged_launch(const PagedAttnArgs& a, const PagedPlan& p, int i, hipStream_t s);
 
+constexpr long kMaxGrid = 0xffffffffl / 256;      // workgroups of a launch: 32 bits count its threads
+
 #ifdef __HIPCC__
 // Rows a .. a + n - 1 and key count of sequence s, as clamped.
 struct SeqRows { int a, n, keys; };
@@ -86,8 +88,8 @@ __device__ __forceinline__ int row_seq(const PagedRows& r, int t) {
     s += (int)__popcll(__ballot(s0 + lane < r.n_seqs && r.row_start[min(s0 + lane, r.n_seqs - 1) + 1] <= t));
   return s;
 }
-// Block `blk` of the sequences' blocks, laid end to end, of `per` items of n * mul + add(s)
-// each; see the users.  All 64 lanes must be active.  f(s): items of sequence s.
+// Item `blk` of the sequences' items laid end to end, f(s) of them for sequence s: item `in` of
+// sequence s (false: there are fewer).  All 64 lanes must be active.
 template <typename F>
 __device__ __forceinline__ bool find_block(int n_seqs, int blk, F&& f, int& s, int& in) {
   const int lane = threadIdx.x & 63;
@@ -105,7 +107,7 @@ __device__ __forceinline__ bool find_block(int n_seqs, int blk, F&& f, int& s, i
       const int l = __builtin_ctzll(m);
       s = s0 + l;
       in = blk - base - __builtin_amdgcn_readlane(inc - own, l);
-      return true;
+      return (unsigned)in < (unsigned)__builtin_amdgcn_readlane(own, l);   // (not of sums past 32 bits)
     }
     base += __builtin_amdgcn_readlane(inc, 63);
   }

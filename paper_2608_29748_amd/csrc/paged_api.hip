@@ -106,7 +106,8 @@ static int attn_args(const rt_paged_kv* kv, const rt_attn_args* g, bool tensors,
   if (g->prefix_len < 0 || g->prefix_len % kPage || g->prefix_len > cap)
     return fail(RT_ERR_INVALID, "prefix_len must be a multiple of 16 within the page table");
   if (!(g->scale >= 0.f) || !isfinite(g->scale)) return fail(RT_ERR_INVALID, "scale must be finite and not negative");
-  const int esz = kv->dtype == RT_BF16 ? 2 : 4, cols = g->n_q_heads * kv->head_dim;
+  const int esz = kv->dtype == RT_BF16 ? 2 : 4;
+  const int64_t cols = (int64_t)g->n_q_heads * kv->head_dim;
   if (tensors && g->n_rows > 0) {
     if ((st = check_tensor("q", g->q, g->ldq, cols, esz))) return st;
     if ((st = check_tensor("out", g->out, g->ldo, cols, esz))) return st;

@@ -167,7 +167,7 @@ hipError_t paged_append(const AppendArgs& a, hipStream_t s) {
   const int vpw = 1024 / r.head_dim, wpg = r.head_dim / 32;
   const long units = a.q ? (long)r.n_rows * ((r.n_q_heads + vpw - 1) / vpw) : 0;
   const long grid = n_kv + (units + wpg - 1) / wpg;
-  if (grid > 0x7fffffffl) return hipErrorInvalidValue;
+  if (grid > kMaxGrid) return hipErrorInvalidValue;
   if (r.head_dim == 128) RT_LAUNCH((append_kernel<T, S, 128>), dim3((unsigned)grid), dim3(256), 0, s, a, (int)n_kv);
   else RT_LAUNCH((append_kernel<T, S, 64>), dim3((unsigned)grid), dim3(128), 0, s, a, (int)n_kv);
   return hipGetLastError();

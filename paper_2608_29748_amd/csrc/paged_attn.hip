@@ -19,7 +19,8 @@ namespace rt {
 typedef __attribute__((address_space(4))) const int32_t const_i32_t;
 
 constexpr int kStep = 32;                  // keys per step of a wave: two pages
-constexpr int kMaxParts = 32;              // key splits of a pass
+constexpr int kMaxParts = 32;              // key splits of a pass, where the other may have as many
+constexpr int kMaxMerge = 64;              // partial results of a row: one a lane of the merge
 constexpr float kMrefInit = -1.0e30f;      // running maximum before any visible key (log2 units)
 
 // A pass of a call: over the shared prefix, or over the sequences' own keys (all of them where no
@@ -795,25 +796,33 @@ static long row_blocks(const PagedAttnArgs& a, bool shared, int rb) {
 static long rows_of(const PagedAttnArgs& a, bool shared) {
   return (long)(shared ? a.r.n_rows : a.max_rows) * (a.r.n_q_heads / a.r.n_kv_heads);
 }
-// Query tiles of a wave of the rows kernel: two where fp32 rows make many blocks and the registers
-// hold them, so that a page is read half as often.
-static int rows_nt(const PagedAttnArgs& a, int elem_bytes) {
-  const PagedRows& r = a.r;
-  return elem_bytes == 4 && r.head_dim == 64 && rows_of(a, false) > 16 &&
-                 row_blocks(a, false, 16) * r.n_kv_heads > 2048 ? 2 : 1;
-}
-// bf16 passes of more than 16 (token, head) rows a block take the tile kernel.
-static bool tiled(const PagedAttnArgs& a, bool shared, int elem_bytes) {
-  return elem_bytes == 2 && rows_of(a, shared) > 16;
-}
-static int block_size(const PagedAttnArgs& a, bool shared, int elem_bytes) {
-  return tiled(a, shared, elem_bytes) ? kTileRows : 16 * rows_nt(a, elem_bytes);
-}
-
 // Keys of a sequence that a pass from key `first` on reads, as far as the host knows.
 static long keys_of(const PagedAttnArgs& a, long first) {
   const long keys = a.max_kv - first, seen = (long)a.window + a.sinks + a.max_rows;
   return a.window > 0 && keys > seen ? seen : keys < 0 ? 0 : keys;
+}
+// Query tiles of a wave of the rows kernel: two where fp32 rows make blocks enough to fill the chip
+// with half as many, each page then being read half as often (4 heads of 64 over 2, 16 rows a sequence
+// behind 1000 keys: 50 sequences 25.1 us with one tile and 26.3 with two, 100 38.4 and 35.3, 200 72.7 and
+// 53.2).  Head_dim 128 would not leave the registers for it.
+static int rows_nt(const PagedAttnArgs& a, int elem_bytes) {
+  const PagedRows& r = a.r;
+  return elem_bytes == 4 && r.head_dim == 64 && rows_of(a, false) > 16 &&
+                 row_blocks(a, false, 16) * r.n_kv_heads > 512 ? 2 : 1;
+}
+// Whether a pass (the sequences' own: from key `first` on) takes the tile kernel: bf16 rows that
+// fill more than one block of 16 and, of the own pass, whose blocks would read more than 160 MB of
+// pages between them (40e6 places of K and V).  Below that the rows kernel, whose waves share a block's
+// keys, ends sooner.  32 heads over 8 of 128, blocks of 16 tokens, rows against tiles: 4 sequences behind 300
+// keys (5e6) 8.2 us, 15.3; 16 behind 300 (21e6) 12.1, 16.5; 4 behind 2048 (34e6) 19.6, 21.6; 8 behind 2048
+// (68e6) 29.3, 24.7; 32 behind 2048 92.8, 66.5.
+static bool tiled(const PagedAttnArgs& a, bool shared, long first, int elem_bytes) {
+  const PagedRows& r = a.r;
+  if (elem_bytes != 2 || rows_of(a, shared) <= 16) return false;
+  return shared || (double)row_blocks(a, false, 16) * r.n_kv_heads * r.head_dim * keys_of(a, first) > 40e6;
+}
+static int block_size(const PagedAttnArgs& a, bool shared, long first, int elem_bytes) {
+  return tiled(a, shared, first, elem_bytes) ? kTileRows : 16 * rows_nt(a, elem_bytes);
 }
 // Whether the rows kernel's pages come by non-temporal loads: where each is read by one workgroup
 // and all of them may be more than twice the 256 MB memory-side cache (64 steps over 4100 keys, 1.08
@@ -821,7 +830,8 @@ static long keys_of(const PagedAttnArgs& a, long first) {
 // MB: 58.2 us against 54.4 with plain loads).
 static bool streamed(const PagedAttnArgs& a, long first, int elem_bytes) {
   const PagedRows& r = a.r;
-  return a.prefix <= first && 2.0 * r.n_seqs * keys_of(a, first) * r.n_kv_heads * r.head_dim * elem_bytes > 512e6;
+  return a.prefix <= first && rows_of(a, false) <= 16 &&
+         2.0 * r.n_seqs * keys_of(a, first) * r.n_kv_heads * r.head_dim * elem_bytes > 512e6;
 }
 
 PagedPlan paged_plan(const PagedAttnArgs& a, int elem_bytes) {
@@ -835,20 +845,26 @@ PagedPlan paged_plan(const PagedAttnArgs& a, int elem_bytes) {
   // 34.0; 32 behind 2048 (260 MB) 39.9, 35.1; 16 behind 8192 55.8, 36.7.
   const double pre = 2.0 * a.prefix * r.n_kv_heads * r.head_dim * elem_bytes;
   const bool apart = a.prefix > 0 && rows_of(a, false) < kTileRows && (r.n_seqs - 1) * pre > 230e6;
+  const long first = apart ? a.prefix : 0;
   auto pick = [&](bool shared, long keys) {
-    const long units = row_blocks(a, shared, block_size(a, shared, elem_bytes)) * r.n_kv_heads;
+    const bool tile = tiled(a, shared, first, elem_bytes);
+    const long units = row_blocks(a, shared, block_size(a, shared, first, elem_bytes)) * r.n_kv_heads;
+    // two workgroups for each of the 256 compute units; more than 32 parts, which a merge then reads,
+    // only as far as the chip is half filled by them (one step over 131072 keys of two KV heads: 56.8 us with
+    // 32, 40.4 with 64; of eight 87.1 and 89.5)
     long s = 512 / units;
+    if (s > kMaxParts) s = apart || 128 / units < kMaxParts ? kMaxParts : 128 / units;
     // keys of a split: enough for its start and its part to be small beside them.  Over a prefix of 8192
     // keys, whose parts are written and read for every row of the batch (64 steps, 32 heads): splits
     // of 256, 512, 1024 and 2048 keys 63.6, 54.4, 48.1 and 61.3 us.
     // Up to 640 keys of rows go without a merge (577 keys, four sequences: 10.6 us in one launch, 11.5 in
     // two; 1028 keys, one sequence: 15.3 and 11.6).
-    long most = keys / (!tiled(a, shared, elem_bytes) ? 8 * kStep : shared ? 16 * kChunkT : 8 * kChunkT);
-    if (!shared && !tiled(a, shared, elem_bytes) && keys <= 640) most = 1;
+    long most = keys / (!tile ? 8 * kStep : shared ? 16 * kChunkT : 8 * kChunkT);
+    if (!shared && !tile && keys <= 640) most = 1;
     if (s > most) s = most;
-    return (int)(s < 1 ? 1 : s > kMaxParts ? kMaxParts : s);
+    return (int)(s < 1 ? 1 : s > kMaxMerge ? kMaxMerge : s);
   };
-  p.splits = pick(false, keys_of(a, apart ? a.prefix : 0));
+  p.splits = pick(false, keys_of(a, first));
   if (apart) p.shared = pick(true, a.prefix);
   return p;
 }
@@ -867,18 +883,18 @@ static hipError_t launch_hd(const PagedAttnArgs& a, const PagedPlan& p, int i, h
     RT_LAUNCH((paged_merge_kernel<T, HD>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p.parts());
     return hipGetLastError();
   }
-  const long E = sizeof(T);
-  const bool t0 = p.shared && tiled(a, true, E), t1 = tiled(a, false, E);
-  const long g0 = p.shared ? row_blocks(a, true, block_size(a, true, E)) * p.shared * r.n_kv_heads : 0;
-  const long g1 = row_blocks(a, false, block_size(a, false, E)) * p.splits * r.n_kv_heads;
+  const long E = sizeof(T), first = p.shared ? a.prefix : 0;
+  const bool t0 = p.shared && tiled(a, true, first, E), t1 = tiled(a, false, first, E);
+  const long g0 = p.shared ? row_blocks(a, true, block_size(a, true, first, E)) * p.shared * r.n_kv_heads : 0;
+  const long g1 = row_blocks(a, false, block_size(a, false, first, E)) * p.splits * r.n_kv_heads;
   if (g0 + g1 <= 0) return hipSuccess;
-  if (g0 + g1 > 0x7fffffffl) return hipErrorInvalidValue;
+  if (g0 + g1 > kMaxGrid || (p.parts() && ((long)r.n_rows * r.n_q_heads + 3) / 4 > kMaxGrid)) return hipErrorInvalidValue;
   const PagedPass p0{1, 0, p.shared, 0, (int)g0};
-  const PagedPass p1{0, p.shared ? a.prefix : 0, p.splits, p.parts() ? p.shared : -1, (int)g1};
+  const PagedPass p1{0, (int)first, p.splits, p.parts() ? p.shared : -1, (int)g1};
   const dim3 gd((unsigned)(g0 + g1));
   const bool ntl = streamed(a, p1.first, E);
   if constexpr (sizeof(T) == 2) {
-    if (t1) {          // (rows that fill tiles of their own fill them over the prefix too)
+    if (t1) {          // (more than 16 rows of a sequence: the prefix is in tiles too)
       // a workgroup that has a compute unit to itself takes twice the stages
       if (g0 + g1 <= 256) RT_LAUNCH((paged_tile_kernel<HD, 4>), gd, dim3(256), 0, s, a, p0, p1);
       else RT_LAUNCH((paged_tile_kernel<HD, 2>), gd, dim3(256), 0, s, a, p0, p1);

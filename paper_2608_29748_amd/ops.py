@@ -3,7 +3,7 @@ position rotation on the way, attention with a sliding window and sinks, and att
 batch whose sequences share a prefix.
 
 Marshalling only.  Work is enqueued on the current stream of the tensors' device; nothing is
-synchronised, and a call may be captured into a graph.  Tensors whose memory another stream
+synchronised, a call may be captured into a graph, and nothing is recorded for gradients.  Tensors whose memory another stream
 made or reuses need the usual event or record_stream, as with any torch call.
 """
 from __future__ import annotations
@@ -75,6 +75,12 @@ def _seqs(cache: PagedKV, kv_len: torch.Tensor, row_start: Optional[torch.Tensor
                                   or row_start.shape[0] != n + 1 or not row_start.is_contiguous()):
         raise _invalid("row_start is a contiguous int32 vector of one more entry than kv_len")
     return n
+
+
+def _counts(**values: int) -> None:
+    for name, x in values.items():
+        if not 0 <= x < 1 << 31:
+            raise _invalid(f"{name} must be in [0, 2^31), not {x}")
 
 
 def _ptr(t: Optional[torch.Tensor]) -> int:
@@ -149,6 +155,7 @@ def kv_append(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, kv_len: torch.Te
 def _attention(call, cache, q, kv_len, window, sinks, prefix_len, row_start, max_rows, max_kv, scale, out, workspace):
     n = _seqs(cache, kv_len, row_start)
     _on(cache, q, kv_len, row_start, out, workspace)
+    _counts(window=window, sinks=sinks, prefix_len=prefix_len, max_rows=max_rows, max_kv=max_kv)
     ldq = _row_stride("q", q, cache.head_dim)
     if q.dtype is not cache.dtype:
         raise _invalid("q has the cache's dtype")
@@ -164,6 +171,8 @@ def _attention(call, cache, q, kv_len, window, sinks, prefix_len, row_start, max
                           max_rows, max_kv, window, sinks, prefix_len, scale)
     desc = cache.desc
     if workspace is not None:
+        if not workspace.is_contiguous():
+            raise _invalid("the workspace must be contiguous")
         _launch(cache, call, desc, args, workspace.data_ptr(), workspace.numel() * workspace.element_size())
         return out
     need = _lib.rt_attn_workspace_bytes(desc, args)

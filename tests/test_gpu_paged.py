@@ -265,6 +265,21 @@ def test_prefix_unseen_places(ops, rows):
     check(attend(ops, c, prefix=96), ref, tol)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("heads,rows,keys", [((4, 2, 64), [1, 3], [300, 90]), ((8, 1, 128), [1], [4100]),
+                                             ((8, 8, 128), [300], [2200])], ids=repr)
+def test_scores_far_below_zero(ops, dtype, heads, rows, keys):
+    """Equal scores weigh alike however low they are (-2^23 and -1.4 times that), as those of zero do."""
+    c = Case(rows, keys, heads, dtype, seed=4)
+    c.kp[:] = 2.0 ** 10
+    c.q_full[:] = 0
+    for w, k in ((40, 3), (5000, 0)):
+        ref, tol = ref_attention(c, w, k)
+        c.q_full[:] = -2.0 ** 10
+        check(attend(ops, c, w, k), ref, tol)
+        c.q_full[:] = 0
+
+
 def test_many_sequences(ops):
     """More sequences than a wave has lanes, some without rows."""
     rows = [i % 3 for i in range(150)]
@@ -375,6 +390,24 @@ def test_two_streams_at_once(ops):
     torch.cuda.synchronize()
     for a, b in got:
         assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+
+
+@pytest.mark.parametrize("heads,keys,splits", [((8, 1, 128), 40000, 64), ((4, 2, 64), 17000, 64), ((8, 8, 128), 40000, 32)],
+                         ids=repr)
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_long_sequences_in_many_parts(ops, heads, keys, splits, dtype):
+    c = Case([1], [keys], heads, dtype, seed=2, ragged=False)
+    parts = c.n * c.hq * splits
+    assert workspace_bytes(ops, c, 0) == -(-parts * c.hd * 4 // 256) * 256 + -(-parts * 8 // 256) * 256
+    check(attend(ops, c, prefix=0), *ref_attention(c))
+
+
+@pytest.mark.parametrize("seqs,rows,keys", [(1, 16, 300), (4, 24, 700), (1, 64, 2100), (2, 64, 2100), (9, 16, 2040)])
+def test_blocks_by_rows_and_by_tiles(ops, seqs, rows, keys):
+    """More than 16 (token, head) rows a sequence, on either side of the size from which on they go in tiles."""
+    c = Case([rows] * seqs, [keys + 17 * i for i in range(seqs)], (32, 8, 128), BF, seed=rows, ragged=seqs > 2)
+    check(attend(ops, c, prefix=0), *ref_attention(c))
+    check(attend(ops, c, 350, 4), *ref_attention(c, 350, 4))
 
 
 @pytest.mark.parametrize("heads,dtype,seqs,prefix,rows", [

@@ -118,6 +118,13 @@ def test_calls_without_rows_do_nothing():
     assert B.rt_attn_workspace_bytes(cache(), attn(out=0, **none)) == 0
 
 
+def test_more_workgroups_than_a_launch_has():
+    rows = dict(n_seqs=1, n_rows=(1 << 28) - 1)
+    refused(B.RT_ERR_CAPACITY, B.rt_kv_append, cache(), append(**rows))
+    refused(B.RT_ERR_CAPACITY, B.rt_window_attention, cache(dtype=B.RT_F32), attn(**rows))
+    refused(B.RT_ERR_CAPACITY, B.rt_prefix_attention, cache(dtype=B.RT_F32), attn(window=0, sinks=0, **rows))
+
+
 def test_workspace_is_of_the_counts_alone():
     kv = cache(max_pages=4096)
     g = dict(n_seqs=3, n_rows=3, max_kv=60000, window=30000, sinks=0)
@@ -161,6 +168,11 @@ def test_tensor_checks():
     no(ops.window_attention, rows, n, 16, out=rows.float())
     no(ops.window_attention, rows[:1].expand(2, 2, 64)[:, :, ::2], n, 16)
     no(ops.prefix_attention, rows, n, 8)
+    no(ops.window_attention, rows, n, (1 << 32) + 5)
+    no(ops.window_attention, rows, n, 16, 1 << 31)
+    no(ops.window_attention, rows, n, 16, max_kv=-1)
+    no(ops.prefix_attention, rows, n, 1 << 32)
+    no(ops.prefix_attention, rows, n, 16, workspace=torch.zeros(64, 64)[:, ::2])
 
 
 def test_rope_table_is_the_rounds_table():
