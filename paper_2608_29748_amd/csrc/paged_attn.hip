@@ -78,6 +78,36 @@ __device__ __forceinline__ RowRange lane_range(const PagedAttnArgs& a, const Pag
   }
   return row_range(a, ps, (long)q.keys - q.n + (tok - q.a), q.keys);
 }
+// Which of the eight keys from key b on a row does not see, a bit each; and the score of key x of
+// such a set, minus infinity where its bit is set.
+__device__ __forceinline__ uint32_t hidden8(const RowRange& r, int b) {
+  auto below = [&](int x) { return (1u << min(max(x - b, 0), 8)) - 1; };
+  return 0xffu & ~(below(r.hi) & (~below(r.lo) | below(r.snk)));
+}
+__device__ __forceinline__ float hide(float s, uint32_t hidden, int x) {
+  const uint32_t m = (uint32_t)((int)(hidden << (31 - x)) >> 31);
+  return __uint_as_float((m & 0xff800000u) | (~m & __float_as_uint(s)));
+}
+// Whether any element that the wave holds is infinite or NaN: the largest exponent, by integer maxima.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+struct Finite {
+  u16x2 top16 = {0, 0};
+  uint32_t top32 = 0;
+  __device__ __forceinline__ void add(const Frag<bf16_t>& f) { add(f.v); }
+  __device__ __forceinline__ void add(const bf16x8& v) {
+    const u32x4 u = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top16 = __builtin_elementwise_max(top16, __builtin_bit_cast(u16x2, u[i] & 0x7fff7fffu));
+  }
+  __device__ __forceinline__ void add(const Frag<float>& f) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top32 = max(top32, __float_as_uint(f.get(i)) & 0x7fffffffu);
+  }
+  __device__ __forceinline__ bool all() const {
+    return __ballot(max(top16[0], top16[1]) >= 0x7f80 || top32 >= 0x7f800000u) == 0;
+  }
+};
 // Sequence and row block of block blk, of `per` (token, head) rows each; false: none.  The results
 // are the same for every lane and made scalar, so that page ids come by scalar loads.
 __device__ __forceinline__ bool block_rows(const PagedAttnArgs& a, bool shared, int blk, int per, int& s, int& rb,
@@ -241,14 +271,17 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, const PagedPas
     // them in a product, so where rows differ in what they see they are added one by one
     uint32_t bad = 0;
     if (!whole) {
-      uint32_t mine = 0;
+      Finite fin;
 #pragma unroll
-      for (int h = 0; h < NHT; ++h)
+      for (int h = 0; h < NHT; ++h) fin.add(f.v[h]);
+      if (!fin.all()) {
+        uint32_t mine = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) mine |= (__builtin_isfinite(f.v[h].get(e)) ? 0u : 1u) << e;
+        for (int h = 0; h < NHT; ++h)
 #pragma unroll
-      for (int x = 1; x < 16; x <<= 1) mine |= __shfl_xor((int)mine, x, 64);
-      if (__ballot(mine != 0)) {
+          for (int e = 0; e < 8; ++e) mine |= (__builtin_isfinite(f.v[h].get(e)) ? 0u : 1u) << e;
+#pragma unroll
+        for (int x = 1; x < 16; x <<= 1) mine |= __shfl_xor((int)mine, x, 64);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (mine >> e & 1)
@@ -268,13 +301,9 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, const PagedPas
         mma(sc[1], f.k[1][ks], qf[t][ks]);
       }
       if (!whole) {
-        const bool ok = g4 < 2 ? f.ok0 : f.ok1;
+        const uint32_t hid = (g4 < 2 ? f.ok0 : f.ok1) ? hidden8(rg[t], k0 + 8 * g4) : 0xffu;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int j = k0 + 8 * g4 + e;
-          const bool vis = ok && j < rg[t].hi && (j >= rg[t].lo || j < rg[t].snk);
-          sc[e >> 2][e & 3] = vis ? sc[e >> 2][e & 3] : -INFINITY;
-        }
+        for (int e = 0; e < 8; ++e) sc[e >> 2][e & 3] = hide(sc[e >> 2][e & 3], hid, e);
       }
       float mx = sc[0][0];
 #pragma unroll
@@ -394,7 +423,6 @@ constexpr int kTileRows = 128;
 constexpr int kChunkT = 64;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 // Wave-wide copies of a page of N KiB at src (the same for every lane) into LDS at dst: copy j brings
 // the 16 bytes at off[j] + j * step of every lane to dst + 1024 j + 16 lane.  Buffer copies: after a
@@ -567,26 +595,33 @@ __device__ __forceinline__ void tile_body(const PagedAttnArgs& a, const PagedPas
 #pragma unroll
     for (int u = 0; u < PAGES; ++u) pages_ok = pages_ok && ok_page(here.id[u]);
     const bool whole = pages_ok && k0 + kChunkT <= min_hi && (k0 >= max_lo || k0 + kChunkT <= min_snk);
-    unsigned bad = 0;                                   // bit 8 page + e: key 16 page + 8 g + e, see below
+    unsigned bad = 0;                                   // bit 8 page + e: key 16 page + 8 g + e
     if (!whole) {
+      uint32_t hid = 0;
 #pragma unroll
-      for (int x = 0; x < 32; ++x) {
-        const int j = k0 + (x >> 3) * kPage + 8 * g + (x & 7);
-        const bool vis = ok_page(here.id[x >> 3]) && j < rg.hi && (j >= rg.lo || j < rg.snk);
-        sc[x >> 4][x & 15] = vis ? sc[x >> 4][x & 15] : -INFINITY;
-      }
+      for (int u = 0; u < PAGES; ++u)
+        hid |= (ok_page(here.id[u]) ? hidden8(rg, k0 + u * kPage + 8 * g) : 0xffu) << (8 * u);
+#pragma unroll
+      for (int x = 0; x < 32; ++x) sc[x >> 4][x & 15] = hide(sc[x >> 4][x & 15], hid, x);
       // keys with a non-finite V element somewhere: a weight of zero must not meet them in a
       // product, so where rows differ in what they see they are added one by one
+      Finite fin;
 #pragma unroll 1
       for (int d = 0; d < NDT; ++d)
 #pragma unroll
-        for (int pg = 0; pg < PAGES; ++pg) {
-          const bf16x8 v = *reinterpret_cast<const bf16x8*>(sm + vad + pg * PGB + d * 1024);
+        for (int pg = 0; pg < PAGES; ++pg) fin.add(*reinterpret_cast<const bf16x8*>(sm + vad + pg * PGB + d * 1024));
+      if (!fin.all()) {
+#pragma unroll 1
+        for (int d = 0; d < NDT; ++d)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) bad |= ((v[e] & 0x7f80) == 0x7f80 ? 1u : 0u) << (8 * pg + e);
-        }
+          for (int pg = 0; pg < PAGES; ++pg) {
+            const bf16x8 v = *reinterpret_cast<const bf16x8*>(sm + vad + pg * PGB + d * 1024);
 #pragma unroll
-      for (int x = 1; x < 32; x <<= 1) bad |= (unsigned)__shfl_xor((int)bad, x, 64);
+            for (int e = 0; e < 8; ++e) bad |= ((v[e] & 0x7f80) == 0x7f80 ? 1u : 0u) << (8 * pg + e);
+          }
+#pragma unroll
+        for (int x = 1; x < 32; x <<= 1) bad |= (unsigned)__shfl_xor((int)bad, x, 64);
+      }
     }
     float m4[4], mx;
 #pragma unroll
@@ -796,9 +831,10 @@ static long row_blocks(const PagedAttnArgs& a, bool shared, int rb) {
 static long rows_of(const PagedAttnArgs& a, bool shared) {
   return (long)(shared ? a.r.n_rows : a.max_rows) * (a.r.n_q_heads / a.r.n_kv_heads);
 }
-// Keys of a sequence that a pass from key `first` on reads, as far as the host knows.
-static long keys_of(const PagedAttnArgs& a, long first) {
-  const long keys = a.max_kv - first, seen = (long)a.window + a.sinks + a.max_rows;
+// Keys that `tokens` consecutive rows of a sequence read in a pass from key `first` on, as far as
+// the host knows.
+static long keys_of(const PagedAttnArgs& a, long first, long tokens) {
+  const long keys = a.max_kv - first, seen = (long)a.window + a.sinks + (tokens < a.max_rows ? tokens : a.max_rows);
   return a.window > 0 && keys > seen ? seen : keys < 0 ? 0 : keys;
 }
 // Query tiles of a wave of the rows kernel: two where fp32 rows make blocks enough to fill the chip
@@ -819,7 +855,7 @@ static int rows_nt(const PagedAttnArgs& a, int elem_bytes) {
 static bool tiled(const PagedAttnArgs& a, bool shared, long first, int elem_bytes) {
   const PagedRows& r = a.r;
   if (elem_bytes != 2 || rows_of(a, shared) <= 16) return false;
-  return shared || (double)row_blocks(a, false, 16) * r.n_kv_heads * r.head_dim * keys_of(a, first) > 40e6;
+  return shared || (double)row_blocks(a, false, 16) * r.n_kv_heads * r.head_dim * keys_of(a, first, 16) > 40e6;
 }
 static int block_size(const PagedAttnArgs& a, bool shared, long first, int elem_bytes) {
   return tiled(a, shared, first, elem_bytes) ? kTileRows : 16 * rows_nt(a, elem_bytes);
@@ -831,20 +867,20 @@ static int block_size(const PagedAttnArgs& a, bool shared, long first, int elem_
 static bool streamed(const PagedAttnArgs& a, long first, int elem_bytes) {
   const PagedRows& r = a.r;
   return a.prefix <= first && rows_of(a, false) <= 16 &&
-         2.0 * r.n_seqs * keys_of(a, first) * r.n_kv_heads * r.head_dim * elem_bytes > 512e6;
+         2.0 * r.n_seqs * keys_of(a, first, a.max_rows) * r.n_kv_heads * r.head_dim * elem_bytes > 512e6;
 }
 
 PagedPlan paged_plan(const PagedAttnArgs& a, int elem_bytes) {
   const PagedRows& r = a.r;
   PagedPlan p{1, 0};
   // A pass over the shared prefix of its own pays where the sequences' rows do not fill tiles by
-  // themselves and reading the prefix once for each would move over 230 MB more than reading it once.
-  // In one pass against two, 8 KV heads of 128: single tokens of 8 sequences behind 4096 keys (117 MB)
-  // 18.7 us, 26.6; 8 behind 8192 (235 MB) 28.2, 27.0; 64 behind 1024 (264 MB) 32.8, 32.4; 16 behind 8192
-  // (503 MB) 47.4, 28.6.  Blocks of 16 tokens: 16 behind 2048 (126 MB) 29.3, 33.4; 8 behind 8192 34.9,
-  // 34.0; 32 behind 2048 (260 MB) 39.9, 35.1; 16 behind 8192 55.8, 36.7.
+  // themselves and reading the prefix once for each would move over 60 MB more than reading it once.
+  // In one pass against two, 8 KV heads of 128: single tokens of 8 sequences behind 2048 keys (59 MB)
+  // 13.8 us, 13.9; 8 behind 4096 18.6, 14.7; 16 behind 4096 28.9, 15.8; 64 behind 1024 32.4, 23.7.  Blocks of
+  // 16 tokens: 4 behind 4096 (50 MB) 20.9, 20.6; 16 behind 1024 (63 MB) 21.4, 21.6; 16 behind 2048 27.1, 23.4;
+  // 32 behind 2048 38.9, 31.5; with 4 KV heads of 64, 32 behind 1024 (33 MB) 14.5, 17.0.
   const double pre = 2.0 * a.prefix * r.n_kv_heads * r.head_dim * elem_bytes;
-  const bool apart = a.prefix > 0 && rows_of(a, false) < kTileRows && (r.n_seqs - 1) * pre > 230e6;
+  const bool apart = a.prefix > 0 && rows_of(a, false) < kTileRows && (r.n_seqs - 1) * pre > 60e6;
   const long first = apart ? a.prefix : 0;
   auto pick = [&](bool shared, long keys) {
     const bool tile = tiled(a, shared, first, elem_bytes);
@@ -854,17 +890,22 @@ PagedPlan paged_plan(const PagedAttnArgs& a, int elem_bytes) {
     // 32, 40.4 with 64; of eight 87.1 and 89.5)
     long s = 512 / units;
     if (s > kMaxParts) s = apart || 128 / units < kMaxParts ? kMaxParts : 128 / units;
-    // keys of a split: enough for its start and its part to be small beside them.  Over a prefix of 8192
-    // keys, whose parts are written and read for every row of the batch (64 steps, 32 heads): splits
-    // of 256, 512, 1024 and 2048 keys 63.6, 54.4, 48.1 and 61.3 us.
-    // Up to 640 keys of rows go without a merge (577 keys, four sequences: 10.6 us in one launch, 11.5 in
-    // two; 1028 keys, one sequence: 15.3 and 11.6).
-    long most = keys / (!tile ? 8 * kStep : shared ? 16 * kChunkT : 8 * kChunkT);
+    long most = keys / (tile ? 4 * kChunkT : 8 * kStep);
+    if (shared && tile) {
+      // Over the prefix a part is written and read for every row of the batch, 0.3 us per 2^17 elements,
+      // while a split takes 1.3 us a chunk: the sum of both is least at the root below; up to the time that
+      // the sequences' own keys take beside it a split costs nothing.
+      const double part = 0.3 / (1 << 17) * r.n_rows * r.n_q_heads * r.head_dim;
+      const double own = 1e-6 / 5 * r.n_seqs * keys_of(a, first, a.max_rows) * r.n_kv_heads * r.head_dim * elem_bytes;
+      const double chunks = fmin(16, fmax(4, fmax(sqrt(keys / (double)kChunkT * part / 1.3), own / 1.3)));
+      most = (long)(keys / (kChunkT * chunks) + 0.5);
+    }
+    // (577 keys, four sequences of a token: 10.6 us in one launch, 11.5 in two; 1028 keys of one: 15.3 and 11.6)
     if (!shared && !tile && keys <= 640) most = 1;
     if (s > most) s = most;
     return (int)(s < 1 ? 1 : s > kMaxMerge ? kMaxMerge : s);
   };
-  p.splits = pick(false, keys_of(a, first));
+  p.splits = pick(false, keys_of(a, first, block_size(a, false, first, elem_bytes) * r.n_kv_heads / r.n_q_heads + 1));
   if (apart) p.shared = pick(true, a.prefix);
   return p;
 }
