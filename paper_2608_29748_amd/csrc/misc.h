@@ -72,8 +72,8 @@ void ar_commit(int32_t* state, const uint64_t* tkeys, const int32_t* sampled, in
                int32_t* step, hipStream_t s);
 void set_ints(int32_t* dst, int n, int v0, int v1, int v2, int v3, hipStream_t s);
 // Round state and first tokens of sequences seq0 .. seq0+n-1 after their prompts (lengths
-// off[s+1] - off[s], behind `share` positions of sequence 0's for the others): the argmax keys[i] of sequence seq0+i, or, with sampled (may be null),
-// the drawn token sampled[seq0+i].
+// off[s+1] - off[s], behind `share` positions of sequence 0's for the others): the argmax keys[i] of
+// sequence seq0+i, or, with sampled (may be null), the drawn token sampled[seq0+i].
 void first_tokens(int32_t* state, int seq0, int n, const uint64_t* keys, const int32_t* sampled, const int32_t* off,
                   int share, int budget, int32_t* first_out, hipStream_t s);
 // out[i] = row off[seq0+i+1] - 1 - g0 of x: the last prompt rows of n consecutive sequences

@@ -93,7 +93,7 @@ static int kv_append(const rt_paged_kv* kv, const rt_append_args* g, hipStream_t
                                            : paged_append<bf16_t, bf16_t>(a, s), "rt_kv_append");
 }
 
-// Checks an attention call and fills the launch arguments.  need_rows: tensors are checked too.
+// Checks an attention call and fills the launch arguments.  tensors: q and out are checked too.
 static int attn_args(const rt_paged_kv* kv, const rt_attn_args* g, bool tensors, PagedAttnArgs* out) {
   int st = check_cache(kv);
   if (st) return st;

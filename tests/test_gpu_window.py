@@ -213,3 +213,21 @@ def test_a_batch_large_enough_for_the_prefix_pass(name, seqs, prefix, window):
         assert (ta[same, 0] == ts[same, 0]).mean() > 0.9
     for e in (apart, shared):
         e.close()
+
+
+@pytest.mark.parametrize("window", [0, 24])
+def test_sampled_rounds_behind_a_shared_prefix(window):
+    """Draws depend on the seed, the sequence and the round alone: the same tokens as apart."""
+    wl, W, prompts = _setup("tiny-f32", batch=3, temperature=1.0)
+    pre, own = prompts[0][:40], [p[40 + 3 * i:50 + 5 * i] for i, p in enumerate(prompts)]
+    eng = engine_for(wl, W)
+    if window:
+        eng.set_window(window, 2)
+    got = []
+    for prefill in (lambda: eng.prefill([np.concatenate([pre, p]) for p in own], 40),
+                    lambda: eng.prefill_prefix(pre, own, 40)):
+        first = prefill()
+        rounds = [eng.spec_round() for _ in range(3)]
+        got.append((list(first), [[list(x[s, :n[s]]) for s in range(3)] for x, n, _ in rounds]))
+    assert got[0] == got[1]
+    eng.close()
