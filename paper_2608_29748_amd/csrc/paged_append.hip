@@ -147,14 +147,22 @@ __global__ __launch_bounds__(2 * HD) void append_kernel(AppendArgs a, int n_kv) 
     const int d = threadIdx.x - NT / 2;
     T* dst = (T*)r.v + base + (size_t)d * kPage;
     const S* src = (const S*)a.vs + (long)row0 * a.ldv + (long)kvh * HD + d;   // (slots below lo: not read)
-    if (lo == 0 && hi == kPage) {
-      float v[2][8];
+    if (hi - lo == 1) {
+      dst[lo] = Elem<T>::from_f32(Elem<S>::to_f32(src[(long)lo * a.ldv]));
+      return;
+    }
+    // all rows' elements are under way before the first is stored (8 sequences of 16 rows that end
+    // inside pages: 4.7 us, 5.7 with a loop of loads and stores)
+    float v[2][8];
 #pragma unroll
-      for (int t = 0; t < kPage; ++t) v[t >> 3][t & 7] = Elem<S>::to_f32(src[(long)t * a.ldv]);
+    for (int t = 0; t < kPage; ++t) v[t >> 3][t & 7] = Elem<S>::to_f32(src[(long)min(max(t, lo), hi - 1) * a.ldv]);
+    if (hi - lo == kPage) {
       store8(dst, v[0]);
       store8(dst + 8, v[1]);
     } else {
-      for (int t = lo; t < hi; ++t) dst[t] = Elem<T>::from_f32(Elem<S>::to_f32(src[(long)t * a.ldv]));
+#pragma unroll
+      for (int t = 0; t < kPage; ++t)
+        if (t >= lo && t < hi) dst[t] = Elem<T>::from_f32(v[t >> 3][t & 7]);
     }
   }
 }
