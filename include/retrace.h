@@ -152,8 +152,7 @@ int rt_prefill(rt_model* m, int32_t n_seqs, const int32_t* prompt_lens, const in
  * prompt prefix_ids followed by its prompt_lens[s] (at least 1) own tokens of prompt_ids.  Same
  * meaning as rt_prefill of those prompts, with the prefix computed and kept once: the sequences'
  * page tables share the pages that it fills (16 tokens each; what is left of it is each sequence's own),
- * and rounds and target-only steps read those once for the batch where that pays
- * (rt_prefix_attention).  The next rt_prefill unshares them.  prefix_len + prompt_len + gen_budget +
+ * and target-only steps read those once for the batch where that pays (rt_prefix_attention).  The next rt_prefill unshares them.  prefix_len + prompt_len + gen_budget +
  * block_size must not exceed max_seq_len. */
 int rt_prefill_prefix(rt_model* m, int32_t prefix_len, const int32_t* prefix_ids, int32_t n_seqs,
                       const int32_t* prompt_lens, const int32_t* prompt_ids, int32_t gen_budget, int32_t* first_tokens);

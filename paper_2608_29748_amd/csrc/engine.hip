@@ -366,7 +366,7 @@ struct Engine : EngineBase {
     const int32_t* items = nullptr;
     int n_items = 0;
     // attention over the cache by the paged operators: a window (target layers), or a prefix
-    // whose pages the sequences share
+    // whose pages the sequences share (target-only steps)
     int window = 0, sinks = 0, prefix = 0;
     // prompt pass with a window: its segments, one of each of n_segs consecutive sequences from
     // sequence seg0 on (row offsets in the pass, n_segs + 1 of them; keys up to the segment's end)
@@ -415,11 +415,14 @@ struct Engine : EngineBase {
     return gemm_call(kind, A, lda, q.Mrows, false, W, q.d, Kp, c.M, e, k_logical);
   }
 
-  // Whether a layer's attention is the paged operators': with a window, or where a pass of its own
-  // over the shared prefix pays.  Then their arguments and plan.
+  // Whether a layer's attention is the paged operators': with a window, or in a target-only step where a
+  // pass of its own over the shared prefix pays (0.6B shape, 16 sequences behind 8192 positions: a step 3.48
+  // ms with caches apart, 1.44).  Rounds keep their own kernels, which find the shared pages in
+  // the caches (the same batch: a round 5.04 ms apart, 3.98 shared, 4.35 with the operators).  Then their
+  // arguments and plan.
   bool paged_layer(const LayerCtx& c, PagedAttnArgs* out, PagedPlan* plan) const {
     const Plan& q = p;
-    if (c.window <= 0 && (c.prefix <= 0 || c.blocks)) return false;
+    if (c.window <= 0 && c.prefix <= 0) return false;
     PagedAttnArgs a{};
     PagedRows& r = a.r;
     r.k = c.kc; r.v = c.vc; r.max_pages = q.pages_per_seq; r.n_pages = q.n_pages;
@@ -434,7 +437,7 @@ struct Engine : EngineBase {
       a.max_rows = c.rows_per_seq; a.max_kv = q.T;
     }
     a.q = at<T>(q.qbuf); a.ldq = q.qN; a.out = at<T>(q.attn); a.ldo = 16 * q.Kp_q; a.packed = 1;
-    a.causal = c.causal; a.scale = 1.0f / sqrtf((float)q.hd);
+    a.scale = 1.0f / sqrtf((float)q.hd);
     a.window = c.window; a.sinks = c.sinks; a.prefix = c.window > 0 ? 0 : c.prefix;
     a.part_o = pat<float>(q.opart, q.s_opart); a.part_ml = pat<float>(q.mlpart, q.s_mlpart);
     PagedPlan pl = paged_plan(a, sizeof(T));
@@ -467,16 +470,14 @@ struct Engine : EngineBase {
     if (c.blocks && c.n_blocks == 0) return RT_OK;      // (the last layer of prompts that do not end in this pass)
     for (int i = 0; i < pl.launches(); ++i) {
       double bytes = 0, flops = 0;
-      if (instrumented()) {   // (prompt passes are not instrumented)
+      if (instrumented()) {   // (rounds alone are, whose paged layers are windowed)
         const double E = sizeof(T), rows = (double)c.n_seqs * c.rows_per_seq;
-        double keys = 0, shared_keys = pl.shared ? a.prefix : 0;
-        for (int s = 0; s < c.n_seqs; ++s) {
-          const double n = c.prof_ctx[s] + c.rows_per_seq - shared_keys;
-          keys += a.window > 0 ? fmin(n, (double)a.window + a.sinks + c.rows_per_seq - 1) : n;
-        }
+        double keys = 0;
+        for (int s = 0; s < c.n_seqs; ++s)
+          keys += fmin((double)c.prof_ctx[s] + c.rows_per_seq, (double)a.window + a.sinks + c.rows_per_seq - 1);
         const double parts = rows * q.Hq * (q.hd + 2) * 4.0 * pl.parts(), out = rows * q.qN * E;
-        bytes = i == 0 ? (keys + shared_keys) * 2.0 * q.Hkv * q.hd * E + out + (pl.parts() ? parts : out) : parts + out;
-        flops = i == 0 ? 4.0 * (keys * c.rows_per_seq + shared_keys * rows) * q.Hq * q.hd : 0;
+        bytes = i == 0 ? keys * 2.0 * q.Hkv * q.hd * E + out + (pl.parts() ? parts : out) : parts + out;
+        flops = i == 0 ? 4.0 * keys * c.rows_per_seq * q.Hq * q.hd : 0;
       }
       prof_begin(i == 0 ? RT_K_ATTENTION : RT_K_ATTN_MERGE, bytes, flops);
       HIPCHK(paged_launch<T>(a, pl, i, stream));
@@ -1020,7 +1021,6 @@ struct Engine : EngineBase {
                  at<T>(q.dkc) + (size_t)l * q.cache_layer_elems, at<T>(q.dvc) + (size_t)l * q.cache_layer_elems,
                  nullptr, 0, prof_ctx.data(), 1};
       c.trace = l;
-      c.prefix = shared;
       CHK(layer(dlayer(l), c));
     }
     stage(2);
@@ -1045,7 +1045,7 @@ struct Engine : EngineBase {
                  at<T>(q.kc) + (size_t)l * q.cache_layer_elems, at<T>(q.vc) + (size_t)l * q.cache_layer_elems,
                  slot >= 0 ? at<T>(q.g) : nullptr, slot * q.d, prof_ctx.data(), 1};
       c.trace = q.LD + l;
-      c.window = window; c.sinks = sinks; c.prefix = shared;
+      c.window = window; c.sinks = sinks;
       CHK(layer(tlayer(l), c));
     }
     stage(4);

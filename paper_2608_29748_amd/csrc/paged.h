@@ -38,7 +38,6 @@ struct PagedAttnArgs {
   const void* q; long ldq;       // storage type, head h at column h * head_dim
   void* out; long ldo;           // the same; packed: GEMM-operand layout with group stride ldo
   int packed;
-  int causal;                    // 0: every key of the sequence is visible (no window then)
   float scale;
   int window, sinks;             // key j of the row at position p: j > p - window or j < sinks
   int prefix;                    // keys 0 .. prefix-1 lie in the same pages of every sequence (a

@@ -114,7 +114,7 @@ static int attn_args(const rt_paged_kv* kv, const rt_attn_args* g, bool tensors,
   }
   PagedAttnArgs a{};
   a.r = rows_of(kv, g->n_seqs, g->n_rows, g->n_q_heads, g->row_start, g->kv_len);
-  a.q = g->q; a.ldq = g->ldq; a.out = g->out; a.ldo = g->ldo; a.packed = 0; a.causal = 1;
+  a.q = g->q; a.ldq = g->ldq; a.out = g->out; a.ldo = g->ldo; a.packed = 0;
   a.scale = g->scale > 0.f ? g->scale : 1.0f / sqrtf((float)kv->head_dim);
   a.window = g->window; a.sinks = g->sinks; a.prefix = g->prefix_len;
   a.max_rows = !g->row_start ? a.r.rows_each : g->max_rows > 0 && g->max_rows < g->n_rows ? g->max_rows : g->n_rows;

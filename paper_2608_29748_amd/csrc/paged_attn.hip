@@ -34,10 +34,9 @@ struct PagedPass {
 };
 
 struct RowRange { int lo, hi, snk; };
-__device__ __forceinline__ RowRange row_range(const PagedAttnArgs& a, const PagedPass& ps, long pos, int keys) {
+__device__ __forceinline__ RowRange row_range(const PagedAttnArgs& a, const PagedPass& ps, long pos) {
   const long cap = (long)a.r.max_pages * kPage;
-  long hi = a.causal ? pos + 1 : (long)keys;
-  hi = max(0l, min(hi, ps.shared ? min(cap, (long)a.prefix) : cap));
+  const long hi = max(0l, min(pos + 1, ps.shared ? min(cap, (long)a.prefix) : cap));
   long lo = ps.first;
   if (a.window > 0) lo = max(lo, pos - a.window + 1);
   lo = min(max(lo, 0l), hi);
@@ -76,7 +75,7 @@ __device__ __forceinline__ RowRange lane_range(const PagedAttnArgs& a, const Pag
     q = seq_rows(r, sq);
     if (tok < q.a || tok >= q.a + q.n) return RowRange{0, 0, 0};     // a row of no sequence
   }
-  return row_range(a, ps, (long)q.keys - q.n + (tok - q.a), q.keys);
+  return row_range(a, ps, (long)q.keys - q.n + (tok - q.a));
 }
 // Which of the eight keys from key b on a row does not see, a bit each; and the score of key x of
 // such a set, minus infinity where its bit is set.

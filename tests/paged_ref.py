@@ -85,7 +85,7 @@ class Case:
                     kv_len=self.kv_len.to(device), start=None if self.start is None else self.start.to(device))
 
 
-def ref_attention(c: Case, window=0, sinks=0, scale=None, causal=True):
+def ref_attention(c: Case, window=0, sinks=0, scale=None):
     """(out, bound) [rows][heads][hd] in float64; rows of no sequence: zeros and infinity."""
     scale = scale or 1 / math.sqrt(c.hd)
     G, H = c.hq // c.hkv, half_step(c.dtype)
@@ -99,7 +99,7 @@ def ref_attention(c: Case, window=0, sinks=0, scale=None, causal=True):
         a = c.first(s)
         pos = (c.keys[s] - n + torch.arange(n))[:, None]
         j = torch.arange(K.shape[0])[None]
-        vis = ok[None] & ((j <= pos) if causal else (j >= 0))
+        vis = ok[None] & (j <= pos)
         if window:
             vis = vis & ((j > pos - window) | (j < sinks))
         for h in range(c.hkv):

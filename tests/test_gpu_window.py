@@ -167,8 +167,8 @@ def test_shared_prefix_rounds_match_oracle(name, prefix):
 @pytest.mark.parametrize("name,seqs,prefix,window", [("tiny-f32", 64, 3600, 0), ("mini-bf16", 64, 7200, 0),
                                                      ("mini-bf16", 64, 7200, 300)])
 def test_a_batch_large_enough_for_the_prefix_pass(name, seqs, prefix, window):
-    """64 sequences behind a long prefix, whose attention is one pass over the prefix and one over
-    the rest, against the same prompts prefilled apart: steps and rounds."""
+    """64 sequences behind a long prefix, whose steps' attention is one pass over the prefix and one
+    over the rest, against the same prompts prefilled apart: steps and rounds."""
     wl, W, _ = _setup(name, batch=seqs, prompt_len=(prefix + 60, prefix + 60), new_tokens=40)
     V, tol = wl.target.vocab, TOL[wl.dtype]
     g = np.random.default_rng(3)
@@ -200,9 +200,6 @@ def test_a_batch_large_enough_for_the_prefix_pass(name, seqs, prefix, window):
         if stats is not None:
             launches = {s["kind"]: s["launches"] for s in stats[0]}
             assert launches["attention"] == wl.draft_layers + wl.target.n_layers
-            # (a launch of its own for the rows' keys and queries: the paged operators have the layer)
-            assert launches["attn_merge"] >= wl.draft_layers + (0 if window else wl.target.n_layers)
-            assert launches["qkv_post"] >= wl.draft_layers + wl.target.n_layers
             break
         (ta, na, _), (ts, ns, _) = apart.spec_round(), shared.spec_round()
         for i in np.nonzero(same)[0][::7]:
