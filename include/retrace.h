@@ -273,7 +273,8 @@ typedef struct rt_append_args {
 int rt_kv_append(const rt_paged_kv* kv, const rt_append_args* args, void* hip_stream);
 
 /* Grouped-query attention of the rows over the cache: query head h reads KV head
- * h / (n_q_heads / n_kv_heads).  Sums and softmax statistics are fp32, for scaled scores within
+ * h / (n_q_heads / n_kv_heads).  Sums and softmax statistics are fp32, and the weights of 16-bit
+ * values are kept to within 2^-16 whatever the sizes and hints, for scaled scores within
  * 2^24 of zero (beyond, neighbouring fp32 numbers are more than one apart); rows that see no key, or
  * none with a score above minus infinity, give zeros.  What lies in places of the cache that a row does not
  * see, infinities and NaN included, does not reach its output; what it sees may make it infinite or NaN.

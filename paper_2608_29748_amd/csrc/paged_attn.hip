@@ -328,7 +328,7 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, const PagedPas
         lsum[t] += p[e];
       }
       // weights of 16 bits: the rounding of each and the rounding of what that left over, two
-      // products (the matrix units have nothing else to do while the keys come in)
+      // products, 2^-16 of the weight (the matrix units have nothing else to do while the keys come in)
       Frag<T> ph, pl;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -419,12 +419,11 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, const PagedPas
 // B operand of O^T = V^T P^T as it stands, and V^T's fragments are contiguous 1 KiB reads.  K rows
 // lie in LDS with their 16-byte pieces permuted by the row (the copies' source addresses are), so
 // that the lanes of a K fragment, a row apart, fall on different banks.
-// Weights are rounded once to bf16 before the product with V and summed as rounded, so that a
-// row's weights still add up to one; half the V products of the rows kernel's two-part weights.
-// Bound by power more than by issue slots: a prompt of 16384 tokens with a window of 4096, 32 heads of 128
-// (963 GFLOP), takes 1.01 ms (950 TFLOP/s); without the softmax's arithmetic 0.83, without copies 0.90, matrix
-// instructions alone 0.64.  Blocks of 256 rows and eight waves took 1.00 to 1.10, one wave's products
-// interleaved with the other half's softmax 1.02 to 1.05.
+// Weights meet V in two bf16 parts, as in the rows kernel, so that a call's outputs are as exact by either: one
+// part, an error of 2^-9 of every weight, made the outputs' error 1.4 times that of their own rounding.  A
+// prompt of 16384 tokens with a window of 4096, 32 heads of 128 (963 GFLOP, half as many again with the second
+// part), takes 1.33 ms (725 TFLOP/s; 1.09 PFLOP/s of matrix instructions), with one part 1.01.  Head_dim 64 keeps
+// three workgroups a compute unit for 16 bytes of scratch (8192 tokens, window 2048: 221 us, with two 236).
 constexpr int kTileRows = 128;
 constexpr int kChunkT = 64;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
@@ -650,14 +649,18 @@ __device__ __forceinline__ void tile_body(const PagedAttnArgs& a, const PagedPas
       lsum *= al;
       mref = mn;
     }
-    u32x4 pf[PAGES];                                    // weights of a page's eight keys
+    // weights of a page's eight keys, in two parts as the rows kernel's: their bf16 rounding and
+    // that of what it left over
+    u32x4 pf[PAGES], pl[PAGES];
 #pragma unroll
     for (int x = 0; x < 32; x += 2) {
       const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[x >> 4][x & 15], sl2, -mref));
       const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[(x + 1) >> 4][(x + 1) & 15], sl2, -mref));
-      const bf2 pk = {(__bf16)p0, (__bf16)p1}, one = {(__bf16)1.f, (__bf16)1.f};
-      lsum = __builtin_amdgcn_fdot2_f32_bf16(pk, one, lsum, false);
-      pf[x >> 3][x >> 1 & 3] = __builtin_bit_cast(unsigned, pk);
+      lsum += p0 + p1;
+      const unsigned ph = __builtin_bit_cast(unsigned, bf2{(__bf16)p0, (__bf16)p1});
+      const bf2 pr = {(__bf16)(p0 - __uint_as_float(ph << 16)), (__bf16)(p1 - __uint_as_float(ph & 0xffff0000u))};
+      pf[x >> 3][x >> 1 & 3] = ph;
+      pl[x >> 3][x >> 1 & 3] = __builtin_bit_cast(unsigned, pr);
     }
     late_v();
     const bool any_bad = __ballot(bad != 0) != 0;
@@ -673,10 +676,14 @@ __device__ __forceinline__ void tile_body(const PagedAttnArgs& a, const PagedPas
       }
     }
 #pragma unroll
-    for (int pg = 0; pg < PAGES; ++pg)
+    for (int pg = 0; pg < PAGES; ++pg) {
 #pragma unroll
       for (int d = 0; d < NDT; ++d)
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[pg][d], __builtin_bit_cast(bf16x8, pf[pg]), o[d], 0, 0, 0);
+#pragma unroll
+      for (int d = 0; d < NDT; ++d)
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[pg][d], __builtin_bit_cast(bf16x8, pl[pg]), o[d], 0, 0, 0);
+    }
     next_pages();
     if (!any_bad) continue;
 #pragma unroll 1
@@ -684,11 +691,15 @@ __device__ __forceinline__ void tile_body(const PagedAttnArgs& a, const PagedPas
 #pragma unroll 1
       for (unsigned m = __builtin_amdgcn_readlane((int)bad, 32 * gg); m; m &= m - 1) {
         const int x = __builtin_ctz(m);                 // key 16 (x / 8) + 8 gg + x % 8
-        unsigned u = pf[0][0];
+        unsigned u = pf[0][0], r = pl[0][0];
 #pragma unroll
-        for (int y = 1; y < 16; ++y) u = (x >> 1) == y ? pf[y >> 2][y & 3] : u;
-        u = (unsigned)__shfl((int)u, c32 + 32 * gg, 64);
-        const float pj = __uint_as_float(x & 1 ? u & 0xffff0000u : u << 16);
+        for (int y = 1; y < 16; ++y) {
+          u = (x >> 1) == y ? pf[y >> 2][y & 3] : u;
+          r = (x >> 1) == y ? pl[y >> 2][y & 3] : r;
+        }
+        const float pm = __uint_as_float(x & 1 ? u & 0xffff0000u : u << 16) +
+                         __uint_as_float(x & 1 ? r & 0xffff0000u : r << 16);
+        const float pj = __shfl(pm, c32 + 32 * gg, 64);
         const bf16_t* vj = reinterpret_cast<const bf16_t*>(sm + PAGES * PGB + (x >> 3) * PGB) + 8 * gg + (x & 7);
 #pragma unroll
         for (int d = 0; d < NDT; ++d)
