@@ -684,6 +684,7 @@ __device__ __forceinline__ void tile_body(const PagedAttnArgs& a, const PagedPas
       for (int d = 0; d < NDT; ++d)
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[pg][d], __builtin_bit_cast(bf16x8, pl[pg]), o[d], 0, 0, 0);
     }
+    wait_lds();                    // (this wave's reads of the stage end before the barrier that gives it away)
     next_pages();
     if (!any_bad) continue;
 #pragma unroll 1
@@ -710,6 +711,7 @@ __device__ __forceinline__ void tile_body(const PagedAttnArgs& a, const PagedPas
           }
       }
     }
+    wait_lds();
   }
   {
     const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(lsum), __float_as_uint(lsum), false, false);
