@@ -459,11 +459,28 @@ enum {
   RT_C_ATTN_SLOTS = 0,     /* workgroups per KV head of the attention */
   RT_C_PAGE_POST = 1,      /* 1: q|k|v post-processing by KV page, 0: by row (where attention does not do it) */
   RT_C_PROMPT_ROWS = 2,    /* rows per pass of a prefill of n prompt tokens in all (arg unused) */
+  RT_C_STEP_PREFIX = 4,    /* key splits of the pass that a target-only step of n sequences makes over their arg
+                              shared positions (0: none, the ordinary attention runs) */
   RT_C_GEMM_COLS = 3       /* columns per workgroup of the target GEMM arg (RT_K_GEMM_QKV .. _DOWN, RT_K_LM_HEAD)
                               over n rows of a prompt pass (LM head: a round) on the mid-size kernel; 0 where
                               another kernel runs */
 };
 int rt_debug_choice(const rt_config* cfg, int32_t choice, int32_t n, int32_t arg);
+/* The same for a call of rt_window_attention or rt_prefix_attention, from its counts alone. */
+enum {
+  RT_A_KERNEL = 0,         /* one of the kernels below */
+  RT_A_STREAMED = 1,       /* 1: the pages come by non-temporal loads */
+  RT_A_SPLITS = 2,         /* key splits of the sequences' own keys */
+  RT_A_PREFIX_SPLITS = 3   /* and of the pass over the prefix (0: none) */
+};
+enum {
+  RT_A_ROWS = 1,           /* blocks of 16 (token, head) rows */
+  RT_A_ROWS_PAIRS = 2,     /* two such blocks a workgroup */
+  RT_A_TILES = 3,          /* tiles of 128 rows, two LDS stages */
+  RT_A_TILES_DEEP = 4,     /* and four */
+  RT_A_PREFIX_TILES = 5    /* the prefix in tiles, the sequences' own keys in blocks of 16 rows */
+};
+int rt_debug_attn_choice(const rt_paged_kv* kv, const rt_attn_args* args, int32_t choice);
 
 #ifdef __cplusplus
 }

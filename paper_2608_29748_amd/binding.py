@@ -40,7 +40,9 @@ RT_T_TRACE_TARGET_Q, RT_T_TRACE_TARGET_ATTN, RT_T_TRACE_TARGET_XMID, RT_T_TRACE_
 RT_K_KINDS = 12
 KERNEL_KIND_NAMES = ["gemm_qkv", "gemm_o", "gemm_gate_up", "gemm_down", "gemm_context", "gemm_cond",
                      "attention", "attn_merge", "rmsnorm", "qkv_post", "lm_head", "misc"]
-RT_C_ATTN_SLOTS, RT_C_PAGE_POST, RT_C_PROMPT_ROWS, RT_C_GEMM_COLS = range(4)
+RT_C_ATTN_SLOTS, RT_C_PAGE_POST, RT_C_PROMPT_ROWS, RT_C_GEMM_COLS, RT_C_STEP_PREFIX = range(5)
+RT_A_KERNEL, RT_A_STREAMED, RT_A_SPLITS, RT_A_PREFIX_SPLITS = range(4)
+RT_A_ROWS, RT_A_ROWS_PAIRS, RT_A_TILES, RT_A_TILES_DEEP, RT_A_PREFIX_TILES = range(1, 6)
 STAGE_NAMES = ["condition", "draft", "draft_lm_head", "verify", "verify_lm_head", "accept", "context_append"]
 RT_PROF_STAGES = 7
 
@@ -49,7 +51,7 @@ EXPORTS = ["rt_workspace_bytes", "rt_weight_count", "rt_init_models", "rt_prefil
            "rt_debug_write", "rt_profile_round", "rt_time_kernel", "rt_ar_steps", "rt_debug_read_rows",
            "rt_spec_round_static", "rt_stream_read", "rt_weight_elements", "rt_debug_choice",
            "rt_kv_append", "rt_attn_workspace_bytes", "rt_window_attention", "rt_prefix_attention",
-           "rt_prefill_prefix", "rt_set_window"]
+           "rt_prefill_prefix", "rt_set_window", "rt_debug_attn_choice"]
 
 
 class RetraceError(RuntimeError):
@@ -141,13 +143,14 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.rt_kv_append.argtypes = [kvp, C.POINTER(rt_append_args), P]
     lib.rt_attn_workspace_bytes.argtypes = [kvp, atp]
     lib.rt_attn_workspace_bytes.restype = C.c_size_t
+    lib.rt_debug_attn_choice.argtypes = [kvp, atp, C.c_int32]
     lib.rt_window_attention.argtypes = [kvp, atp, P, C.c_size_t, P]
     lib.rt_prefix_attention.argtypes = [kvp, atp, P, C.c_size_t, P]
     for name in ("rt_init_models", "rt_prefill", "rt_spec_round", "rt_spec_round_forced", "rt_spec_round_static",
                  "rt_stream_read", "rt_destroy",
                  "rt_set_debug", "rt_debug_read", "rt_debug_read_rows", "rt_debug_write", "rt_profile_round",
                  "rt_time_kernel", "rt_ar_steps", "rt_debug_choice", "rt_kv_append", "rt_window_attention",
-                 "rt_prefix_attention", "rt_prefill_prefix", "rt_set_window"):
+                 "rt_prefix_attention", "rt_prefill_prefix", "rt_set_window", "rt_debug_attn_choice"):
         getattr(lib, name).restype = C.c_int
     return lib
 
@@ -336,6 +339,14 @@ def rt_debug_write(h: int, tensor_id: int, seq: int, data: bytes) -> None:
 def rt_debug_choice(cfg: rt_config, choice: int, n: int, arg: int = 0) -> int:
     """What the library would launch (RT_C_*); needs no GPU."""
     v = _lib.rt_debug_choice(C.byref(cfg), choice, n, arg)
+    if v < 0:
+        _check(v)
+    return v
+
+
+def rt_debug_attn_choice(kv: rt_paged_kv, args: rt_attn_args, choice: int) -> int:
+    """What an attention call over a paged cache would launch (RT_A_*); needs no GPU."""
+    v = _lib.rt_debug_attn_choice(kv, args, choice)
     if v < 0:
         _check(v)
     return v

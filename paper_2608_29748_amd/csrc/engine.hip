@@ -226,6 +226,32 @@ static int prompt_pass_rows(const Plan& p, int total) {
   const int n_pass = (total + p.PF - 1) / p.PF;
   return (int)rup((size_t)(total + n_pass - 1) / n_pass, 256);
 }
+// Plan of a paged attention whose parts fit the split buffers (one part always fits: they have a full set of rows
+// for every split of the other kernels).  false: the ordinary attention runs, as it also does where
+// no pass over a shared prefix pays.
+static bool paged_fit(const Plan& q, const PagedAttnArgs& a, PagedPlan* out) {
+  PagedPlan pl = paged_plan(a, q.esz);
+  if (a.window <= 0 && pl.shared == 0) return false;
+  const size_t cap = (q.mlpart - q.opart) / 4, cap_ml = (q.attn_plan - q.mlpart) / 4;
+  size_t ml;
+  while (paged_part_floats(a, pl, &ml) > cap || ml > cap_ml) {
+    if (pl.splits > 1) --pl.splits;
+    else if (pl.shared > 1) --pl.shared;
+    else return false;
+  }
+  *out = pl;
+  return true;
+}
+// Counts of the paged attention over n sequences of `each` rows in a round or step.
+static PagedAttnArgs paged_counts(const Plan& q, int n, int each) {
+  PagedAttnArgs a{};
+  PagedRows& r = a.r;
+  r.max_pages = q.pages_per_seq; r.n_pages = q.n_pages;
+  r.n_q_heads = q.Hq; r.n_kv_heads = q.Hkv; r.head_dim = q.hd;
+  r.n_seqs = n; r.rows_each = each; r.n_rows = n * each;
+  a.max_rows = each; a.max_kv = q.T;
+  return a;
+}
 // Rounds and steps that post-process q|k|v by KV page (a workgroup per page and head, sixteen
 // lanes a row) instead of one wave per row and head.  Enough rows to fill the chip, and enough
 // of a page's sixteen row places in use; us a launch, by row and by page: 4B widths, 1 row a
@@ -423,33 +449,23 @@ struct Engine : EngineBase {
   bool paged_layer(const LayerCtx& c, PagedAttnArgs* out, PagedPlan* plan) const {
     const Plan& q = p;
     if (c.window <= 0 && c.prefix <= 0) return false;
-    PagedAttnArgs a{};
+    PagedAttnArgs a = paged_counts(q, c.n_seqs, c.rows_per_seq);
     PagedRows& r = a.r;
-    r.k = c.kc; r.v = c.vc; r.max_pages = q.pages_per_seq; r.n_pages = q.n_pages;
+    r.k = c.kc; r.v = c.vc;
     r.page_table = c.pt + (size_t)c.seg0 * q.pages_per_seq;
-    r.n_q_heads = q.Hq; r.n_kv_heads = q.Hkv; r.head_dim = q.hd; r.n_rows = c.M;
     if (c.blocks) {
+      r.n_rows = c.M; r.rows_each = 0;
       r.n_seqs = c.n_segs; r.row_start = c.seg_start; r.kv_len = c.seg_keys; r.kv_stride = 1;
       a.max_rows = c.seg_rows; a.max_kv = c.seg_kv;
     } else {
-      r.n_seqs = c.n_seqs; r.rows_each = c.rows_per_seq;
       r.kv_len = c.pos0; r.kv_stride = c.stride; r.kv_add = c.rows_per_seq;
-      a.max_rows = c.rows_per_seq; a.max_kv = q.T;
     }
     a.q = at<T>(q.qbuf); a.ldq = q.qN; a.out = at<T>(q.attn); a.ldo = 16 * q.Kp_q; a.packed = 1;
     a.scale = 1.0f / sqrtf((float)q.hd);
     a.window = c.window; a.sinks = c.sinks; a.prefix = c.window > 0 ? 0 : c.prefix;
     a.part_o = pat<float>(q.opart, q.s_opart); a.part_ml = pat<float>(q.mlpart, q.s_mlpart);
-    PagedPlan pl = paged_plan(a, sizeof(T));
-    if (c.window <= 0 && pl.shared == 0) return false;
-    // (one part always fits: the buffer has a full set of rows for every split of the other kernels)
-    const size_t cap = (q.mlpart - q.opart) / 4, cap_ml = (q.attn_plan - q.mlpart) / 4;
-    size_t ml;
-    while (paged_part_floats(a, pl, &ml) > cap || ml > cap_ml) {
-      if (pl.splits > 1) --pl.splits;
-      else if (pl.shared > 1) --pl.shared;
-      else return false;
-    }
+    PagedPlan pl;
+    if (!paged_fit(q, a, &pl)) return false;
     *out = a;
     *plan = pl;
     return true;
@@ -1850,6 +1866,13 @@ int rt_debug_choice(const rt_config* cfg, int32_t choice, int32_t n, int32_t arg
     return gemm_columns(p, arg, n);
   }
   if (n < 1 || n > p.bmax) return fail(RT_ERR_CAPACITY, "%d sequences outside [1, %d]", n, p.bmax);
+  if (choice == RT_C_STEP_PREFIX) {
+    if (arg < 0 || arg > p.T || arg % kPage) return fail(RT_ERR_INVALID, "%d shared positions", arg);
+    PagedAttnArgs a = paged_counts(p, n, 1);
+    a.prefix = arg;
+    PagedPlan pl;
+    return arg > 0 && paged_fit(p, a, &pl) ? pl.shared : 0;
+  }
   if (arg != 1 && arg != p.bk) return fail(RT_ERR_INVALID, "rows per sequence must be 1 or the block size");
   switch (choice) {
     case RT_C_ATTN_SLOTS: {

@@ -54,6 +54,10 @@ struct PagedPlan {
   int launches() const { return parts() ? 2 : 1; }      // the passes, the merge
 };
 PagedPlan paged_plan(const PagedAttnArgs& a, int elem_bytes);
+// The kernel of a call's passes (RT_A_KERNEL's values), with pages by non-temporal loads or not, and
+// the workgroups of the prefix's pass and of the sequences' own.
+struct PagedChoice { int kernel; bool streamed; long g0, g1; };
+PagedChoice paged_choice(const PagedAttnArgs& a, const PagedPlan& p, int elem_bytes);
 // Floats of part_o (returned) and part_ml.
 size_t paged_part_floats(const PagedAttnArgs& a, const PagedPlan& p, size_t* ml);
 // Launch i (0 .. p.launches() - 1, in order) of a call.

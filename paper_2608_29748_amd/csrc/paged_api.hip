@@ -178,6 +178,27 @@ size_t rt_attn_workspace_bytes(const rt_paged_kv* kv, const rt_attn_args* args) 
   }
 }
 
+int rt_debug_attn_choice(const rt_paged_kv* kv, const rt_attn_args* args, int32_t choice) {
+  try {
+    PagedAttnArgs a;
+    const int st = attn_args(kv, args, false, &a);
+    if (st) return st;
+    if (a.r.n_rows == 0) return fail(RT_ERR_INVALID, "a call without rows launches nothing");
+    const int esz = kv->dtype == RT_BF16 ? 2 : 4;
+    const PagedPlan p = paged_plan(a, esz);
+    const PagedChoice c = paged_choice(a, p, esz);
+    switch (choice) {
+      case RT_A_KERNEL: return c.kernel;
+      case RT_A_STREAMED: return c.streamed;
+      case RT_A_SPLITS: return p.splits;
+      case RT_A_PREFIX_SPLITS: return p.shared;
+      default: return fail(RT_ERR_INVALID, "unknown choice %d", choice);
+    }
+  } catch (...) {
+    return fail(RT_ERR_INVALID, "unexpected exception in rt_debug_attn_choice");
+  }
+}
+
 int rt_window_attention(const rt_paged_kv* kv, const rt_attn_args* args, void* d_workspace, size_t ws_bytes,
                         void* hip_stream) {
   try {

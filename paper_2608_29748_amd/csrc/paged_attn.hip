@@ -12,6 +12,7 @@
 //   prefix      where it pays, keys [0, prefix) in a pass over the rows of all sequences, whose
 //               tiles so fill with rows that read the same pages, and beside it [prefix, p]
 //               sequence by sequence; a merge joins them.
+#include "../../include/retrace.h"
 #include "paged.h"
 
 namespace rt {
@@ -937,6 +938,21 @@ size_t paged_part_floats(const PagedAttnArgs& a, const PagedPlan& p, size_t* ml)
   return rows * a.r.head_dim;
 }
 
+PagedChoice paged_choice(const PagedAttnArgs& a, const PagedPlan& p, int elem_bytes) {
+  const long first = p.shared ? a.prefix : 0;
+  PagedChoice c{};
+  c.g0 = p.shared ? row_blocks(a, true, block_size(a, true, first, elem_bytes)) * p.shared * a.r.n_kv_heads : 0;
+  c.g1 = row_blocks(a, false, block_size(a, false, first, elem_bytes)) * p.splits * a.r.n_kv_heads;
+  // (own rows in tiles: more than 16 rows of a sequence, the prefix is in tiles too; a workgroup that
+  // has a compute unit to itself takes twice the stages)
+  c.kernel = tiled(a, false, first, elem_bytes)              ? c.g0 + c.g1 <= 256 ? RT_A_TILES_DEEP : RT_A_TILES
+             : p.shared && tiled(a, true, first, elem_bytes) ? RT_A_PREFIX_TILES
+             : rows_nt(a, elem_bytes) == 2                   ? RT_A_ROWS_PAIRS
+                                                             : RT_A_ROWS;
+  c.streamed = (c.kernel == RT_A_ROWS || c.kernel == RT_A_PREFIX_TILES) && streamed(a, first, elem_bytes);
+  return c;
+}
+
 template <typename T, int HD>
 static hipError_t launch_hd(const PagedAttnArgs& a, const PagedPlan& p, int i, hipStream_t s) {
   const PagedRows& r = a.r;
@@ -945,35 +961,25 @@ static hipError_t launch_hd(const PagedAttnArgs& a, const PagedPlan& p, int i, h
     RT_LAUNCH((paged_merge_kernel<T, HD>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p.parts());
     return hipGetLastError();
   }
-  const long E = sizeof(T), first = p.shared ? a.prefix : 0;
-  const bool t0 = p.shared && tiled(a, true, first, E), t1 = tiled(a, false, first, E);
-  const long g0 = p.shared ? row_blocks(a, true, block_size(a, true, first, E)) * p.shared * r.n_kv_heads : 0;
-  const long g1 = row_blocks(a, false, block_size(a, false, first, E)) * p.splits * r.n_kv_heads;
-  if (g0 + g1 <= 0) return hipSuccess;
-  if (g0 + g1 > kMaxGrid || (p.parts() && ((long)r.n_rows * r.n_q_heads + 3) / 4 > kMaxGrid)) return hipErrorInvalidValue;
-  const PagedPass p0{1, 0, p.shared, 0, (int)g0};
-  const PagedPass p1{0, (int)first, p.splits, p.parts() ? p.shared : -1, (int)g1};
-  const dim3 gd((unsigned)(g0 + g1));
-  const bool ntl = streamed(a, p1.first, E);
+  const PagedChoice c = paged_choice(a, p, sizeof(T));
+  if (c.g0 + c.g1 <= 0) return hipSuccess;
+  if (c.g0 + c.g1 > kMaxGrid || (p.parts() && ((long)r.n_rows * r.n_q_heads + 3) / 4 > kMaxGrid)) return hipErrorInvalidValue;
+  const PagedPass p0{1, 0, p.shared, 0, (int)c.g0};
+  const PagedPass p1{0, p.shared ? a.prefix : 0, p.splits, p.parts() ? p.shared : -1, (int)c.g1};
+  const dim3 gd((unsigned)(c.g0 + c.g1));
   if constexpr (sizeof(T) == 2) {
-    if (t1) {          // (more than 16 rows of a sequence: the prefix is in tiles too)
-      // a workgroup that has a compute unit to itself takes twice the stages
-      if (g0 + g1 <= 256) RT_LAUNCH((paged_tile_kernel<HD, 4>), gd, dim3(256), 0, s, a, p0, p1);
-      else RT_LAUNCH((paged_tile_kernel<HD, 2>), gd, dim3(256), 0, s, a, p0, p1);
-      return hipGetLastError();
-    }
-    if (t0) {
-      if (ntl) RT_LAUNCH((paged_both_kernel<HD, true>), gd, dim3(256), 0, s, a, p0, p1);
-      else RT_LAUNCH((paged_both_kernel<HD, false>), gd, dim3(256), 0, s, a, p0, p1);
-      return hipGetLastError();
-    }
+    if (c.kernel == RT_A_TILES_DEEP) RT_LAUNCH((paged_tile_kernel<HD, 4>), gd, dim3(256), 0, s, a, p0, p1);
+    else if (c.kernel == RT_A_TILES) RT_LAUNCH((paged_tile_kernel<HD, 2>), gd, dim3(256), 0, s, a, p0, p1);
+    else if (c.kernel == RT_A_PREFIX_TILES && c.streamed) RT_LAUNCH((paged_both_kernel<HD, true>), gd, dim3(256), 0, s, a, p0, p1);
+    else if (c.kernel == RT_A_PREFIX_TILES) RT_LAUNCH((paged_both_kernel<HD, false>), gd, dim3(256), 0, s, a, p0, p1);
+    if (c.kernel != RT_A_ROWS) return hipGetLastError();
   } else if constexpr (HD == 64) {
-    if (rows_nt(a, E) == 2) {
+    if (c.kernel == RT_A_ROWS_PAIRS) {
       RT_LAUNCH((paged_rows_kernel<T, HD, 2, 4, false>), gd, dim3(256), 0, s, a, p0, p1);
       return hipGetLastError();
     }
   }
-  if (ntl) RT_LAUNCH((paged_rows_kernel<T, HD, 1, 4, true>), gd, dim3(256), 0, s, a, p0, p1);
+  if (c.streamed) RT_LAUNCH((paged_rows_kernel<T, HD, 1, 4, true>), gd, dim3(256), 0, s, a, p0, p1);
   else RT_LAUNCH((paged_rows_kernel<T, HD, 1, 4, false>), gd, dim3(256), 0, s, a, p0, p1);
   return hipGetLastError();
 }
