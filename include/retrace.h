@@ -152,7 +152,7 @@ int rt_prefill(rt_model* m, int32_t n_seqs, const int32_t* prompt_lens, const in
  * prompt prefix_ids followed by its prompt_lens[s] (at least 1) own tokens of prompt_ids.  Same
  * meaning as rt_prefill of those prompts, with the prefix computed and kept once: the sequences'
  * page tables share the pages that it fills (16 tokens each; what is left of it is each sequence's own),
- * and target-only steps read those once for the batch where that pays (rt_prefix_attention).  The next rt_prefill unshares them.  prefix_len + prompt_len + gen_budget +
+ * and target-only steps read those once for the batch where that pays (see rt_prefix_attention).  The next rt_prefill unshares them.  prefix_len + prompt_len + gen_budget +
  * block_size must not exceed max_seq_len. */
 int rt_prefill_prefix(rt_model* m, int32_t prefix_len, const int32_t* prefix_ids, int32_t n_seqs,
                       const int32_t* prompt_lens, const int32_t* prompt_ids, int32_t gen_budget, int32_t* first_tokens);
@@ -283,8 +283,10 @@ int rt_kv_append(const rt_paged_kv* kv, const rt_append_args* args, void* hip_st
  * window, its own position included) or j < sinks (the first tokens, which stay visible).
  *
  * rt_prefix_attention: the row at position p sees every key j <= p, and the positions
- * 0 .. prefix_len - 1 (a multiple of 16; 0: none) lie in the same pages for every sequence: they are
- * read once for the whole batch, through the first sequence's page table.
+ * 0 .. prefix_len - 1 (a multiple of 16; 0: none) lie in the same pages for every sequence, and are
+ * found through the first sequence's page table.  A pass of their own reads them once for the whole batch
+ * where that pays: where the sequences have fewer than 128 (row, query head) pairs for a KV head on the average
+ * and reading the prefix once for each would move over 60 MB more.
  *
  * max_rows and max_kv: the most rows and keys of a sequence, as far as the host knows (0: unknown).
  * They only size the split of the work: they must be the same for the call and for its workspace,

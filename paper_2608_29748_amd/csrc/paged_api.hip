@@ -117,7 +117,11 @@ static int attn_args(const rt_paged_kv* kv, const rt_attn_args* g, bool tensors,
   a.q = g->q; a.ldq = g->ldq; a.out = g->out; a.ldo = g->ldo; a.packed = 0;
   a.scale = g->scale > 0.f ? g->scale : 1.0f / sqrtf((float)kv->head_dim);
   a.window = g->window; a.sinks = g->sinks; a.prefix = g->prefix_len;
-  a.max_rows = !g->row_start ? a.r.rows_each : g->max_rows > 0 && g->max_rows < g->n_rows ? g->max_rows : g->n_rows;
+  // (unknown: what a sequence has on the average over as many as can have any)
+  const int n = g->n_seqs < g->n_rows ? g->n_seqs : g->n_rows;
+  a.max_rows = !g->row_start    ? a.r.rows_each
+               : g->max_rows == 0 ? (int)(n > 0 ? ((long)g->n_rows + n - 1) / n : 0)
+                                  : g->max_rows < g->n_rows ? g->max_rows : g->n_rows;
   a.max_kv = (int)(g->max_kv > 0 && g->max_kv < cap ? g->max_kv : cap);
   *out = a;
   return RT_OK;

@@ -849,9 +849,12 @@ static long row_blocks(const PagedAttnArgs& a, bool shared, int rb) {
   if (r.row_start) return (long)r.n_rows * G / rb + r.n_seqs;
   return (long)r.n_seqs * (((long)r.rows_each * G + rb - 1) / rb);
 }
-// Rows of a sequence (of all of them, over the prefix) for a KV head, as far as the host knows.
+// (token, head) rows for a KV head: of all sequences over the prefix, else of a sequence on the average over
+// as many as can have any.  (Not of the longest: one prompt among single tokens does not fill their tiles.)
 static long rows_of(const PagedAttnArgs& a, bool shared) {
-  return (long)(shared ? a.r.n_rows : a.max_rows) * (a.r.n_q_heads / a.r.n_kv_heads);
+  const PagedRows& r = a.r;
+  const long n = shared ? 1 : r.n_seqs < r.n_rows ? r.n_seqs : r.n_rows;
+  return (r.n_rows + n - 1) / n * (r.n_q_heads / r.n_kv_heads);
 }
 // Keys that `tokens` consecutive rows of a sequence read in a pass from key `first` on, as far as
 // the host knows.
@@ -868,7 +871,7 @@ static int rows_nt(const PagedAttnArgs& a, int elem_bytes) {
   return elem_bytes == 4 && r.head_dim == 64 && rows_of(a, false) > 16 &&
                  row_blocks(a, false, 16) * r.n_kv_heads > 512 ? 2 : 1;
 }
-// Whether a pass (the sequences' own: from key `first` on) takes the tile kernel: bf16 rows that
+// Whether a pass (the sequences' own: from key `first` on) takes the tile kernel: bf16 rows that on the average
 // fill more than one block of 16 and, of the own pass, whose blocks would read more than 160 MB of
 // pages between them (40e6 places of K and V).  Below that the rows kernel, whose waves share a block's
 // keys, ends sooner.  32 heads over 8 of 128, blocks of 16 tokens, rows against tiles: 4 sequences behind 300
@@ -888,19 +891,20 @@ static int block_size(const PagedAttnArgs& a, bool shared, long first, int elem_
 // MB: 58.2 us against 54.4 with plain loads).
 static bool streamed(const PagedAttnArgs& a, long first, int elem_bytes) {
   const PagedRows& r = a.r;
-  return a.prefix <= first && rows_of(a, false) <= 16 &&
+  return a.prefix <= first && (long)a.max_rows * (r.n_q_heads / r.n_kv_heads) <= 16 &&
          2.0 * r.n_seqs * keys_of(a, first, a.max_rows) * r.n_kv_heads * r.head_dim * elem_bytes > 512e6;
 }
 
 PagedPlan paged_plan(const PagedAttnArgs& a, int elem_bytes) {
   const PagedRows& r = a.r;
   PagedPlan p{1, 0};
-  // A pass over the shared prefix of its own pays where the sequences' rows do not fill tiles by
+  // A pass over the shared prefix of its own pays where the sequences' rows do not, on the average, fill tiles by
   // themselves and reading the prefix once for each would move over 60 MB more than reading it once.
   // In one pass against two, 8 KV heads of 128: single tokens of 8 sequences behind 2048 keys (59 MB)
   // 13.8 us, 13.9; 8 behind 4096 18.6, 14.7; 16 behind 4096 28.9, 15.8; 64 behind 1024 32.4, 23.7.  Blocks of
   // 16 tokens: 4 behind 4096 (50 MB) 20.9, 20.6; 16 behind 1024 (63 MB) 21.4, 21.6; 16 behind 2048 27.1, 23.4;
   // 32 behind 2048 38.9, 31.5; with 4 KV heads of 64, 32 behind 1024 (33 MB) 14.5, 17.0.
+  // A prompt of 96 rows among 63 tokens, all behind 8192: 394, 58; of 200 among 15 behind 4096 93, 48.
   const double pre = 2.0 * a.prefix * r.n_kv_heads * r.head_dim * elem_bytes;
   const bool apart = a.prefix > 0 && rows_of(a, false) < kTileRows && (r.n_seqs - 1) * pre > 60e6;
   const long first = apart ? a.prefix : 0;

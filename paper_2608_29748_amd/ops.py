@@ -201,7 +201,7 @@ def prefix_attention(cache: PagedKV, q: torch.Tensor, kv_len: torch.Tensor, pref
                      scale: float = 0.0, out: Optional[torch.Tensor] = None,
                      workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Causal attention of the rows q over the cache, whose sequences share the pages of their first
-    prefix_len positions: those are read once for the batch.  See rt_prefix_attention; workspace and
-    out as for window_attention."""
+    prefix_len positions: those are read once for the batch where that pays.  See rt_prefix_attention;
+    workspace and out as for window_attention."""
     return _attention(_lib.rt_prefix_attention, cache, q, kv_len, 0, 0, prefix_len, row_start, max_rows, max_kv, scale,
                       out, workspace)

@@ -261,6 +261,17 @@ def test_prefix_pass_and_pages_outside_the_pool(ops, heads, seqs, each, prefix, 
     compare(ops, c, prefix=prefix, **kw)
 
 
+@gpu
+@pytest.mark.parametrize("heads,dtype", [((16, 8, 128), BF), ((16, 8, 64), BF), ((8, 4, 128), F32)], ids=repr)
+@pytest.mark.parametrize("max_rows", [0, 1, 96])
+def test_one_prompt_among_tokens_behind_a_prefix(ops, heads, dtype, max_rows):
+    rows = [1] * 20 + [96] + [1] * 19 + [0, 2]
+    c = Case(rows, [2048 + r + (11 * s) % 70 for s, r in enumerate(rows)], heads, dtype, seed=7, extra_rows=2, shared=2048)
+    assert choice(c, B.RT_A_PREFIX_SPLITS, prefix=2048, max_rows=max_rows) > 0
+    compare(ops, c, prefix=2048, max_rows=max_rows)
+    compare(ops, c, 300, 4, max_rows=max_rows)
+
+
 def test_the_comparison_sees_what_is_missing():
     """On the host: NaN that should be there and is not, NaN that should not, a number out of bounds."""
     ref, tol = torch.zeros(4, 2, 3, dtype=torch.float64), torch.full((4, 2, 3), 0.1, dtype=torch.float64)

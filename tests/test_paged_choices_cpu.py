@@ -48,6 +48,28 @@ def test_prefix_passes(n, prefix, taken):
         assert choose(B.RT_A_KERNEL, (32, 8, 128), B.RT_BF16, n, n, max_kv=prefix + 500, prefix=prefix) == B.RT_A_PREFIX_TILES
 
 
+@pytest.mark.parametrize("n_seqs,n_rows,max_rows", [(64, 64 - 1 + 96, 96), (64, 64 - 1 + 96, 0), (64, 64, 0), (64, 64, 1),
+                                                    (16, 15 + 200, 200), (64, 8, 0)])
+def test_the_prefix_pass_goes_by_how_full_the_sequences_are(n_seqs, n_rows, max_rows):
+    """One prompt among single tokens, or rows that nobody counted, do not take it away."""
+    kw = dict(max_rows=max_rows, max_kv=8192 + 400, prefix=8192, ragged=True)
+    assert choose(B.RT_A_PREFIX_SPLITS, (32, 8, 128), B.RT_BF16, n_seqs, n_rows, **kw) > 0
+    assert choose(B.RT_A_KERNEL, (32, 8, 128), B.RT_BF16, n_seqs, n_rows, **kw) in (B.RT_A_PREFIX_TILES, B.RT_A_TILES)
+
+
+def test_prompts_fill_tiles_by_themselves():
+    for max_rows in (0, 320):
+        assert choose(B.RT_A_PREFIX_SPLITS, (32, 8, 128), B.RT_BF16, 32, 32 * 208, max_rows=max_rows, max_kv=4500,
+                      prefix=4096, ragged=True) == 0
+
+
+@pytest.mark.parametrize("max_rows", [0, 1])
+def test_steps_that_nobody_counted_are_steps(max_rows):
+    kw = dict(max_rows=max_rows, max_kv=16384, window=4096, sinks=4, ragged=True)
+    assert choose(B.RT_A_KERNEL, (40, 8, 128), B.RT_BF16, 64, 64, **kw) == B.RT_A_ROWS
+    assert choose(B.RT_A_STREAMED, (40, 8, 128), B.RT_BF16, 64, 64, **kw) == 1
+
+
 def step_prefix(name, seqs, prefix, positions):
     wl = get(name, batch=seqs, prompt_len=(positions, positions), new_tokens=40)
     cfg = config_from(wl.target, dtype=wl.dtype, draft_layers=wl.draft_layers, cond_layers=wl.cond_layers,
