@@ -862,14 +862,16 @@ static long keys_of(const PagedAttnArgs& a, long first, long tokens) {
   const long keys = a.max_kv - first, seen = (long)a.window + a.sinks + (tokens < a.max_rows ? tokens : a.max_rows);
   return a.window > 0 && keys > seen ? seen : keys < 0 ? 0 : keys;
 }
-// Query tiles of a wave of the rows kernel: two where fp32 rows make blocks enough to fill the chip
-// with half as many, each page then being read half as often (4 heads of 64 over 2, 16 rows a sequence
-// behind 1000 keys: 50 sequences 25.1 us with one tile and 26.3 with two, 100 38.4 and 35.3, 200 72.7 and
-// 53.2).  Head_dim 128 would not leave the registers for it.
+// Query tiles of a wave of the rows kernel: two where blocks of one tile are more than the 256 compute units, each
+// page then being read half as often.  Blocks, one tile, two, us: 16 rows a sequence behind 1000 keys, 4 heads of 64
+// over 2: 280 35.6 27.4, 400 37.3 32.9, 512 42.1 34.8, 600 53.7 47.2; behind 300 keys, 32 heads over 8: 128 9.5 13.2,
+// 256 10.0 13.5, 320 14.2 13.6, 512 14.6 13.8, 768 19.2 21.1; behind 2000: 128 22.1 23.1, 384 50.6 49.9.  Below 256 a
+// pair of heads behind 1000 keys would gain (200: 25.8 23.0), the others lose.  Head_dim 128 would not leave the
+// registers for it.
 static int rows_nt(const PagedAttnArgs& a, int elem_bytes) {
   const PagedRows& r = a.r;
   return elem_bytes == 4 && r.head_dim == 64 && rows_of(a, false) > 16 &&
-                 row_blocks(a, false, 16) * r.n_kv_heads > 512 ? 2 : 1;
+                 row_blocks(a, false, 16) * r.n_kv_heads > 256 ? 2 : 1;
 }
 // Whether a pass (the sequences' own: from key `first` on) takes the tile kernel: bf16 rows that on the average
 // fill more than one block of 16 and, of the own pass, whose blocks would read more than 160 MB of

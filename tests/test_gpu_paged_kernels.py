@@ -159,7 +159,7 @@ def test_deep_tiles(ops, heads, rows, window, sinks):
     compare(ops, c, window, sinks, **kw)
 
 
-# fp32, head_dim 64, more than 512 blocks of 16 rows: two blocks a workgroup
+# fp32, head_dim 64, more than 256 blocks of 16 rows: two blocks a workgroup
 @gpu
 @pytest.mark.parametrize("ragged", [True, False])
 @pytest.mark.parametrize("window,sinks", [(1, 0), (40, 3), (33, 32), (500, 0)])

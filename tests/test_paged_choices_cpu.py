@@ -33,6 +33,12 @@ def test_kernels(heads, dtype, n_seqs, rows, kv, kernel):
     assert choose(B.RT_A_KERNEL, heads, dtype, n_seqs, n_seqs * rows, max_kv=kv) == kernel
 
 
+@pytest.mark.parametrize("n_seqs,kernel", [(8, B.RT_A_ROWS), (9, B.RT_A_ROWS_PAIRS), (12, B.RT_A_ROWS_PAIRS)])
+def test_pairs_where_single_blocks_outnumber_the_compute_units(n_seqs, kernel):
+    """32 blocks a sequence, 256 compute units."""
+    assert choose(B.RT_A_KERNEL, (32, 8, 64), B.RT_F32, n_seqs, n_seqs * 16, max_kv=316) == kernel
+
+
 def test_streamed_pages():
     for n, want in ((16, 0), (64, 1)):
         assert choose(B.RT_A_STREAMED, (40, 8, 128), B.RT_BF16, n, n, max_kv=4100) == want
