@@ -928,8 +928,13 @@ PagedPlan paged_plan(const PagedAttnArgs& a, int elem_bytes) {
       const double chunks = fmin(16, fmax(4, fmax(sqrt(keys / (double)kChunkT * part / 1.3), own / 1.3)));
       most = (long)(keys / (kChunkT * chunks) + 0.5);
     }
-    // (577 keys, four sequences of a token: 10.6 us in one launch, 11.5 in two; 1028 keys of one: 15.3 and 11.6)
-    if (!shared && !tile && keys <= 640) most = 1;
+    // Parts need a merge of some 3 us, as much as a few steps of a wave: fewer steps are one part.  In fp32 at
+    // head_dim 128 a step is 4096 cycles of matrix instructions, and two parts pay at once.  Four tokens
+    // and 8 KV heads, in parts and as one, us: bf16 of 128, 577 keys 9.9 10.1, 640 9.8 9.9, 768 9.1 11.1, 1028 9.7
+    // 14.4; bf16 of 64, 577 8.8 7.0, 768 8.1 7.4, 900 8.7 8.6, 1028 8.6 9.1; fp32 of 64, 577 12.0 12.2, 640 11.6
+    // 11.8, 768 10.5 13.2; fp32 of 128, 577 18.3 24.1, 768 15.0 28.1.
+    const int few = elem_bytes == 2 ? (r.head_dim == 64 ? 7 : 5) : r.head_dim == 64 ? 5 : 0;
+    if (!shared && !tile && keys <= few * 4 * kStep) most = 1;
     if (s > most) s = most;
     return (int)(s < 1 ? 1 : s > kMaxMerge ? kMaxMerge : s);
   };

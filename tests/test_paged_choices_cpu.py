@@ -39,6 +39,14 @@ def test_pairs_where_single_blocks_outnumber_the_compute_units(n_seqs, kernel):
     assert choose(B.RT_A_KERNEL, (32, 8, 64), B.RT_F32, n_seqs, n_seqs * 16, max_kv=316) == kernel
 
 
+@pytest.mark.parametrize("hd,dtype,one,parts", [(128, B.RT_BF16, 640, 641), (64, B.RT_BF16, 896, 897),
+                                                (64, B.RT_F32, 640, 641), (128, B.RT_F32, 511, 512)])
+def test_few_steps_are_one_part(hd, dtype, one, parts):
+    for window in (0, 5000):
+        n = [choose(B.RT_A_SPLITS, (8, 8, hd), dtype, 4, 4, max_kv=kv, window=window) for kv in (one, parts)]
+        assert n[0] == 1 and n[1] > 1
+
+
 def test_streamed_pages():
     for n, want in ((16, 0), (64, 1)):
         assert choose(B.RT_A_STREAMED, (40, 8, 128), B.RT_BF16, n, n, max_kv=4100) == want
