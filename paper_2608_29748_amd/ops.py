@@ -3,8 +3,9 @@ position rotation on the way, attention with a sliding window and sinks, and att
 batch whose sequences share a prefix.
 
 Marshalling only.  Work is enqueued on the current stream of the tensors' device; nothing is
-synchronised, a call may be captured into a graph, and nothing is recorded for gradients.  Tensors whose memory another stream
-made or reuses need the usual event or record_stream, as with any torch call.
+synchronised, and a call may be captured into a graph.  There are no gradients: outside torch.no_grad() a tensor
+that requires one is refused.  Tensors whose memory another stream made or reuses need the usual event or
+record_stream, as with any torch call.
 """
 from __future__ import annotations
 
@@ -42,7 +43,7 @@ class PagedKV:
         self.device, self.dtype = k.device, k.dtype
         self.index = k.get_device()          # -1: not on a GPU
         self.n_kv_heads, self.head_dim, self.n_tables = h, d, page_table.shape[0]
-        _on(self, v, page_table)
+        _on(self, k, v, page_table)
         self.desc = B.rt_paged_kv(k.data_ptr(), v.data_ptr(), page_table.data_ptr(), n, page_table.shape[1], h, d,
                                   PAGE, _DTYPES[k.dtype])
 
@@ -50,9 +51,19 @@ class PagedKV:
 # (The checks below run on every call of a decoding step, so they are written flat.)
 
 def _on(cache: PagedKV, *tensors) -> None:
+    """Operands on the cache's device, of which none asks for a gradient that no call here records."""
+    index = cache.index
     for t in tensors:
-        if t is not None and t.get_device() != cache.index:
-            raise _invalid(f"a tensor is on {t.device}, the cache on {cache.device}")
+        if t is not None and (t.get_device() != index or t.requires_grad):
+            _operand(cache, t)
+
+
+def _operand(cache: PagedKV, t: torch.Tensor) -> None:
+    if t.get_device() != cache.index:
+        raise _invalid(f"a tensor is on {t.device}, the cache on {cache.device}")
+    if torch.is_grad_enabled():
+        raise _invalid("a tensor requires a gradient, which these operators do not have: detach it, or call under "
+                       "torch.no_grad()")
 
 
 def _row_stride(name: str, t: torch.Tensor, head_dim: int) -> int:

@@ -1,0 +1,58 @@
+"""Operands of the paged-cache operators that a call cannot serve as asked, refused without a GPU."""
+import pytest
+import torch
+
+from paper_2608_29748_amd import binding as B
+from paper_2608_29748_amd import ops
+
+
+def paged(n=4, h=2, d=64, dtype=torch.bfloat16, seqs=2, width=2):
+    return (torch.zeros(n, h, 16, d, dtype=dtype), torch.zeros(n, h, d, 16, dtype=dtype),
+            torch.zeros(seqs, width, dtype=torch.int32))
+
+
+def refusal(call, *a, **kw):
+    with pytest.raises(B.RetraceError) as e:
+        call(*a, **kw)
+    assert e.value.code == B.RT_ERR_INVALID
+    return str(e.value)
+
+
+@pytest.mark.parametrize("which", ["q", "k", "v", "q_norm", "k_norm", "q_out", "rope"])
+def test_gradients_are_not_lost_silently_by_an_append(which):
+    c, n = ops.PagedKV(*paged()), torch.zeros(2, dtype=torch.int32)
+    t = dict(q=torch.zeros(2, 2, 64), k=torch.zeros(2, 2, 64), v=torch.zeros(2, 2, 64), q_norm=torch.ones(64).bfloat16(),
+             k_norm=torch.ones(64).bfloat16(), q_out=torch.zeros(2, 2, 64).bfloat16(), rope=torch.zeros(2, 32, 32))
+
+    def call():
+        ops.kv_append(c, t["k"], t["v"], n, q=t["q"], q_out=t["q_out"], rope=t["rope"], q_norm=t["q_norm"],
+                      k_norm=t["k_norm"])
+
+    assert "not on a GPU" in refusal(call)
+    t[which].requires_grad_(True)
+    assert "gradient" in refusal(call)
+    with torch.no_grad():
+        assert "not on a GPU" in refusal(call)       # (served, on a GPU)
+
+
+@pytest.mark.parametrize("which", ["q", "out"])
+def test_gradients_are_not_lost_silently_by_attention(which):
+    c, n = ops.PagedKV(*paged()), torch.zeros(2, dtype=torch.int32)
+    t = dict(q=torch.zeros(2, 2, 64).bfloat16(), out=torch.zeros(2, 2, 64).bfloat16())
+    calls = (lambda: ops.window_attention(c, t["q"], n, 16, out=t["out"]), lambda: ops.prefix_attention(c, t["q"], n, 16, out=t["out"]))
+    for call in calls:
+        assert "not on a GPU" in refusal(call)
+    t[which].requires_grad_(True)
+    for call in calls:
+        assert "gradient" in refusal(call)
+        with torch.no_grad():
+            assert "not on a GPU" in refusal(call)
+
+
+def test_caches_that_require_gradients():
+    for i in (0, 1):
+        t = list(paged())
+        t[i].requires_grad_(True)
+        assert "gradient" in refusal(ops.PagedKV, *t)
+        with torch.no_grad():
+            ops.PagedKV(*t)
