@@ -301,7 +301,7 @@ typedef struct rt_attn_args {
   int32_t n_seqs, n_rows, n_q_heads, max_rows, max_kv;
   int32_t window, sinks;   /* rt_window_attention (0 elsewhere) */
   int32_t prefix_len;      /* rt_prefix_attention (0 elsewhere) */
-  float scale;             /* of the scores; 0: 1 / sqrt(head_dim) */
+  float scale;             /* of the scores, a normal number; 0: 1 / sqrt(head_dim) */
 } rt_attn_args;
 /* Bytes of device workspace (256-byte aligned) that a call with these arguments needs, from the
  * counts alone: q and out may be NULL.  0 where it needs none, and for invalid arguments (see

@@ -1,5 +1,6 @@
 // C entries of the paged-cache operators: argument checks (before any device work) and launches.
 #include <hip/hip_runtime.h>
+#include <float.h>
 #include <math.h>
 
 #include "host.h"
@@ -106,6 +107,7 @@ static int attn_args(const rt_paged_kv* kv, const rt_attn_args* g, bool tensors,
   if (g->prefix_len < 0 || g->prefix_len % kPage || g->prefix_len > cap)
     return fail(RT_ERR_INVALID, "prefix_len must be a multiple of 16 within the page table");
   if (!(g->scale >= 0.f) || !isfinite(g->scale)) return fail(RT_ERR_INVALID, "scale must be finite and not negative");
+  if (g->scale > 0.f && g->scale < FLT_MIN) return fail(RT_ERR_INVALID, "scale is below the smallest normal number");
   const int esz = kv->dtype == RT_BF16 ? 2 : 4;
   const int64_t cols = (int64_t)g->n_q_heads * kv->head_dim;
   if (tensors && g->n_rows > 0) {

@@ -167,6 +167,8 @@ def _attention(call, cache, q, kv_len, window, sinks, prefix_len, row_start, max
     n = _seqs(cache, kv_len, row_start)
     _on(cache, q, kv_len, row_start, out, workspace)
     _counts(window=window, sinks=sinks, prefix_len=prefix_len, max_rows=max_rows, max_kv=max_kv)
+    if 0.0 < scale < 2.0 ** -126:               # (which float32 may round to 0, the default scale)
+        raise _invalid("scale is below the smallest normal number")
     ldq = _row_stride("q", q, cache.head_dim)
     if q.dtype is not cache.dtype:
         raise _invalid("q has the cache's dtype")

@@ -56,3 +56,16 @@ def test_caches_that_require_gradients():
         assert "gradient" in refusal(ops.PagedKV, *t)
         with torch.no_grad():
             ops.PagedKV(*t)
+
+
+@pytest.mark.parametrize("scale", [1e-40, 1e-46, 1e-60])
+def test_a_scale_that_float32_loses_is_not_the_default(scale):
+    """The C entry sees a denormal number or, from Python, what would have become 0."""
+    c, n, q = ops.PagedKV(*paged()), torch.zeros(2, dtype=torch.int32), torch.zeros(2, 2, 64).bfloat16()
+    assert "scale" in refusal(ops.window_attention, c, q, n, 16, scale=scale)
+    assert "scale" in refusal(ops.prefix_attention, c, q, n, 16, scale=scale)
+    assert "not on a GPU" in refusal(ops.window_attention, c, q, n, 16, scale=2.0 ** -126)
+    if scale > 1e-45:
+        kv = B.rt_paged_kv(1 << 20, 1 << 20, 1 << 20, 4, 2, 2, 64, 16, B.RT_BF16)
+        g = B.rt_attn_args(1 << 20, 128, 1 << 20, 128, 0, 1 << 20, 2, 2, 2, 0, 0, 16, 0, 0, scale)
+        assert "scale" in refusal(B.rt_window_attention, kv, g)
