@@ -71,7 +71,7 @@ def _row_stride(name: str, t: torch.Tensor, head_dim: int) -> int:
     st = t.stride()
     if len(st) != 3 or t.shape[2] != head_dim:
         raise _invalid(f"{name} is [rows][heads][{head_dim}], not {tuple(t.shape)}")
-    if (st[2] != 1 or st[1] != head_dim) and t.numel():
+    if (st[2] != 1 or (st[1] != head_dim and t.shape[1] != 1)) and t.numel():
         raise _invalid(f"the heads of a row of {name} must lie one after the other")
     return st[0] if t.shape[0] > 1 else t.shape[1] * head_dim
 

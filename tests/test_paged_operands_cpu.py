@@ -69,3 +69,13 @@ def test_a_scale_that_float32_loses_is_not_the_default(scale):
         kv = B.rt_paged_kv(1 << 20, 1 << 20, 1 << 20, 4, 2, 2, 64, 16, B.RT_BF16)
         g = B.rt_attn_args(1 << 20, 128, 1 << 20, 128, 0, 1 << 20, 2, 2, 2, 0, 0, 16, 0, 0, scale)
         assert "scale" in refusal(B.rt_window_attention, kv, g)
+
+
+def test_one_head_has_no_head_stride():
+    """Rows of a single head, however the dimension of size one came about."""
+    c, n = ops.PagedKV(*paged(h=1)), torch.zeros(2, dtype=torch.int32)
+    one = torch.zeros(2, 64, 1).bfloat16().transpose(1, 2)
+    assert one.stride(1) != 64
+    assert "not on a GPU" in refusal(ops.kv_append, c, one, one, n, q=one)
+    assert "not on a GPU" in refusal(ops.window_attention, c, one, n, 16, out=one.clone(memory_format=torch.preserve_format))
+    assert "one after the other" in refusal(ops.window_attention, c, torch.zeros(2, 64, 2).bfloat16().transpose(1, 2), n, 16)
