@@ -862,16 +862,18 @@ static long keys_of(const PagedAttnArgs& a, long first, long tokens) {
   const long keys = a.max_kv - first, seen = (long)a.window + a.sinks + (tokens < a.max_rows ? tokens : a.max_rows);
   return a.window > 0 && keys > seen ? seen : keys < 0 ? 0 : keys;
 }
-// Query tiles of a wave of the rows kernel: two where blocks of one tile are more than the 256 compute units, each
-// page then being read half as often.  Blocks, one tile, two, us: 16 rows a sequence behind 1000 keys, 4 heads of 64
-// over 2: 280 35.6 27.4, 400 37.3 32.9, 512 42.1 34.8, 600 53.7 47.2; behind 300 keys, 32 heads over 8: 128 9.5 13.2,
-// 256 10.0 13.5, 320 14.2 13.6, 512 14.6 13.8, 768 19.2 21.1; behind 2000: 128 22.1 23.1, 384 50.6 49.9.  Below 256 a
-// pair of heads behind 1000 keys would gain (200: 25.8 23.0), the others lose.  Head_dim 128 would not leave the
-// registers for it.
+// Query tiles of a wave of the rows kernel: two where blocks of one tile are more than the 256 compute units and
+// read more than 28 steps of keys, each page then being read half as often.  One tile, two, us: 16 rows a sequence of 4
+// heads of 64 over 2 behind 1000 keys 320 blocks 36.0 27.2, 640 54.9 47.0, 1400 109 95; behind 2000 400 65.5 51.6,
+// 640 105 90.  32 heads over 8: behind 1000 320 blocks 29.2 26.1, 512 30.0 32.6, 768 42.3 45.4, 1024 53.3 46.4; behind
+// 2000 320 49.9 38.1, 768 74.8 81.5, 1024 99.9 83.1.  Fewer blocks or keys gain less than they lose: behind
+// 1000 192 21.1 19.3, 256 22.4 21.5; behind 700 320 22.6 25.4, 640 31.6 34.9, 1024 41.2 35.9; behind 300 256 10.1
+// 13.6, 512 14.4 13.7, 768 18.9 21.1; a window of 128 320 11.5 11.6, 640 14.2 16.2, 800 18.1 16.2.  Head_dim 128 would
+// not leave the registers for it.
 static int rows_nt(const PagedAttnArgs& a, int elem_bytes) {
   const PagedRows& r = a.r;
   return elem_bytes == 4 && r.head_dim == 64 && rows_of(a, false) > 16 &&
-                 row_blocks(a, false, 16) * r.n_kv_heads > 256 ? 2 : 1;
+                 row_blocks(a, false, 16) * r.n_kv_heads > 256 && keys_of(a, 0, 16) > 28 * kStep ? 2 : 1;
 }
 // Whether a pass (the sequences' own: from key `first` on) takes the tile kernel: bf16 rows that on the average
 // fill more than one block of 16 and, of the own pass, whose blocks would read more than 160 MB of

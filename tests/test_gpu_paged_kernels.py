@@ -159,13 +159,13 @@ def test_deep_tiles(ops, heads, rows, window, sinks):
     compare(ops, c, window, sinks, **kw)
 
 
-# fp32, head_dim 64, more than 256 blocks of 16 rows: two blocks a workgroup
+# fp32, head_dim 64, more than 256 blocks of 16 rows and more than 896 keys: two blocks a workgroup
 @gpu
 @pytest.mark.parametrize("ragged", [True, False])
-@pytest.mark.parametrize("window,sinks", [(1, 0), (40, 3), (33, 32), (500, 0)])
+@pytest.mark.parametrize("window,sinks", [(897, 0), (900, 3), (929, 33), (5000, 0)])
 def test_pairs_of_row_blocks(ops, ragged, window, sinks):
-    rows = [(7 * s) % 31 for s in range(64)] if ragged else [16] * 64
-    c = Case(rows, [r + (13 * s) % 90 for s, r in enumerate(rows)], (32, 8, 64), F32, seed=window, ragged=ragged,
+    rows = [(7 * s) % 31 for s in range(12)] if ragged else [16] * 12
+    c = Case(rows, [r + (197 * s) % 1100 for s, r in enumerate(rows)], (32, 8, 64), F32, seed=window, ragged=ragged,
              extra_rows=2 * ragged)
     reach(c, B.RT_A_ROWS_PAIRS, window=window, sinks=sinks)
     compare(ops, c, window, sinks)
@@ -174,28 +174,29 @@ def test_pairs_of_row_blocks(ops, ragged, window, sinks):
 @gpu
 @pytest.mark.parametrize("value", [math.nan, math.inf])
 def test_pairs_and_what_no_row_sees(ops, value):
-    rows = [16 + s % 3 for s in range(64)]
-    keys = [r + (13 * s) % 90 for s, r in enumerate(rows)]
-    c = junk(small_scores(Case(rows, keys, (32, 8, 64), F32, seed=2, fill=value)), 20, 3, value)
-    reach(c, B.RT_A_ROWS_PAIRS, window=20, sinks=3)
-    compare(ops, c, 20, 3)
-    wild = [(s, keys[s] - 1 - s % 20, s % 64) for s in range(0, 64, 5)] + [(7, 1, 3)]
+    rows = [16 + s % 3 for s in range(12)]
+    keys = [r + (197 * s) % 1100 for s, r in enumerate(rows)]
+    window, sinks = 890, 3
+    c = junk(small_scores(Case(rows, keys, (32, 8, 64), F32, seed=2, fill=value)), window, sinks, value)
+    reach(c, B.RT_A_ROWS_PAIRS, window=window, sinks=sinks)
+    compare(ops, c, window, sinks)
+    wild = [(s, keys[s] - 1 - s % 20, s % 64) for s in range(0, 12, 3)] + [(5, 1, 3), (5, 95, 9), (4, 40, 60)]
     for s, j, d in wild:
         page, slot = c.place(s, j)
         c.vp[page, :, d, slot] = value
-    c.table[9, 0] = -1
-    compare(ops, c, 20, 3, wild=wild)
+    c.table[8, 0] = c.table[10, 30] = -1
+    compare(ops, c, window, sinks, wild=wild)
 
 
 @gpu
 def test_pairs_behind_a_prefix(ops):
-    rows = [16 + s % 3 for s in range(64)]
-    keys = [320 + r + s % 40 for s, r in enumerate(rows)]
-    keys[5] = 300
-    c = Case(rows, keys, (32, 8, 64), F32, seed=4, shared=320, extra_rows=2)
-    c.table[5, :20] = c.table[0, :20]
-    reach(c, B.RT_A_ROWS_PAIRS, prefix=320, prefix_splits=True)
-    compare(ops, c, prefix=320)
+    rows = [16 + s % 3 for s in range(20)]
+    keys = [912 + r + s % 40 for s, r in enumerate(rows)]
+    keys[5] = 900
+    c = Case(rows, keys, (32, 8, 64), F32, seed=4, shared=912, extra_rows=2)
+    c.table[5, :57] = c.table[0, :57]
+    reach(c, B.RT_A_ROWS_PAIRS, prefix=912, prefix_splits=True)
+    compare(ops, c, prefix=912)
 
 
 # pages by non-temporal loads: more than 512 MB of them, as far as the host knows

@@ -28,15 +28,17 @@ def test_choices_are_checked():
     ((32, 8, 128), B.RT_BF16, 16, 16, 300, B.RT_A_ROWS), ((32, 8, 128), B.RT_BF16, 32, 16, 700, B.RT_A_TILES),
     ((32, 8, 128), B.RT_BF16, 1, 500, 490, B.RT_A_TILES_DEEP), ((32, 8, 128), B.RT_BF16, 1, 16384, 16384, B.RT_A_TILES),
     ((32, 8, 128), B.RT_BF16, 64, 1, 16384, B.RT_A_ROWS), ((32, 8, 128), B.RT_F32, 4, 4096, 4096, B.RT_A_ROWS),
-    ((32, 8, 64), B.RT_F32, 64, 16, 200, B.RT_A_ROWS_PAIRS), ((32, 8, 64), B.RT_F32, 4, 16, 200, B.RT_A_ROWS)], ids=repr)
+    ((32, 8, 64), B.RT_F32, 64, 16, 2000, B.RT_A_ROWS_PAIRS), ((32, 8, 64), B.RT_F32, 4, 16, 2000, B.RT_A_ROWS)], ids=repr)
 def test_kernels(heads, dtype, n_seqs, rows, kv, kernel):
     assert choose(B.RT_A_KERNEL, heads, dtype, n_seqs, n_seqs * rows, max_kv=kv) == kernel
 
 
-@pytest.mark.parametrize("n_seqs,kernel", [(8, B.RT_A_ROWS), (9, B.RT_A_ROWS_PAIRS), (12, B.RT_A_ROWS_PAIRS)])
-def test_pairs_where_single_blocks_outnumber_the_compute_units(n_seqs, kernel):
-    """32 blocks a sequence, 256 compute units."""
-    assert choose(B.RT_A_KERNEL, (32, 8, 64), B.RT_F32, n_seqs, n_seqs * 16, max_kv=316) == kernel
+@pytest.mark.parametrize("n_seqs,kv,window,kernel", [
+    (8, 1016, 0, B.RT_A_ROWS), (9, 1016, 0, B.RT_A_ROWS_PAIRS), (9, 897, 0, B.RT_A_ROWS_PAIRS), (9, 896, 0, B.RT_A_ROWS),
+    (9, 4000, 128, B.RT_A_ROWS), (9, 4000, 1000, B.RT_A_ROWS_PAIRS)])
+def test_pairs_where_single_blocks_outnumber_the_compute_units(n_seqs, kv, window, kernel):
+    """32 blocks a sequence, 256 compute units; and enough keys."""
+    assert choose(B.RT_A_KERNEL, (32, 8, 64), B.RT_F32, n_seqs, n_seqs * 16, max_kv=kv, window=window) == kernel
 
 
 @pytest.mark.parametrize("hd,dtype,one,parts", [(128, B.RT_BF16, 640, 641), (64, B.RT_BF16, 896, 897),
