@@ -285,8 +285,8 @@ int rt_kv_append(const rt_paged_kv* kv, const rt_append_args* args, void* hip_st
  * rt_prefix_attention: the row at position p sees every key j <= p, and the positions
  * 0 .. prefix_len - 1 (a multiple of 16; 0: none) lie in the same pages for every sequence, and are
  * found through the first sequence's page table.  A pass of their own reads them once for the whole batch
- * where that pays: where the sequences have fewer than 128 (row, query head) pairs for a KV head on the average
- * and reading the prefix once for each would move over 60 MB more.
+ * where that pays: where the sequences have fewer than 128 (row, query head) pairs (fp32: 16) for a KV head on the
+ * average and reading the prefix once for each would move over 60 MB more, and 56 bytes more for every element of out.
  *
  * max_rows and max_kv: the most rows and keys of a sequence, as far as the host knows (0: unknown).
  * They only size the split of the work: they must be the same for the call and for its workspace,

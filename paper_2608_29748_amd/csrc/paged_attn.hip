@@ -903,14 +903,20 @@ PagedPlan paged_plan(const PagedAttnArgs& a, int elem_bytes) {
   const PagedRows& r = a.r;
   PagedPlan p{1, 0};
   // A pass over the shared prefix of its own pays where the sequences' rows do not, on the average, fill tiles by
-  // themselves and reading the prefix once for each would move over 60 MB more than reading it once.
-  // In one pass against two, 8 KV heads of 128: single tokens of 8 sequences behind 2048 keys (59 MB)
-  // 13.8 us, 13.9; 8 behind 4096 18.6, 14.7; 16 behind 4096 28.9, 15.8; 64 behind 1024 32.4, 23.7.  Blocks of
-  // 16 tokens: 4 behind 4096 (50 MB) 20.9, 20.6; 16 behind 1024 (63 MB) 21.4, 21.6; 16 behind 2048 27.1, 23.4;
-  // 32 behind 2048 38.9, 31.5; with 4 KV heads of 64, 32 behind 1024 (33 MB) 14.5, 17.0.
-  // A prompt of 96 rows among 63 tokens, all behind 8192: 394, 58; of 200 among 15 behind 4096 93, 48.
+  // themselves and reading the prefix once for each would move over 60 MB more than reading it once, and 56 bytes
+  // more for every element of the rows' outputs: two parts of 4 bytes are written and read, and count
+  // 3.5 times, since what is read again mostly lies in caches.  In one pass against two, us, 8 KV heads of 128: single
+  // tokens, four query heads each, 8 sequences behind 2048 keys (59 MB) 13.1, 13.7; 8 behind 4096 17.8, 14.5; 16 behind
+  // 4096 28.1, 15.5; 64 behind 1024 27.6, 18.2.  Blocks of 16 tokens: 4 behind 4096 (50 MB) 24.0, 22.6; 16 behind 1024
+  // (63) 25.4, 24.6; 32 behind 1024 (130) 38.0, 38.4; 64 behind 1024 (264) 50.3, 62.3; 16 behind 2048 34.2, 30.1; 32
+  // behind 2048 55.9, 52.0; 16 behind 4096 52.5, 47.4.  Heads of 64: 64 behind 1024 (132) 38.2, 50.6; 16 behind 4096
+  // 40.2, 32.7; 8 heads over 4, 64 behind 1024 (66) 14.7, 20.7; 64 behind 4096 50.6, 35.4.
+  // A prompt of 96 rows among 63 tokens, all behind 8192: 394, 58; of 200 among 15 behind 4096 93, 48.  In fp32 the pass
+  // goes in blocks of 16, which 16 pairs fill: 8 KV heads of 64 with four query heads each, 64 behind 1024, one token
+  // 34.0, 21.6, 16 tokens 93, 117; 32 behind 2048, four tokens 35.2, 34.9; 4 KV heads with two, four tokens 22.3, 17.5.
   const double pre = 2.0 * a.prefix * r.n_kv_heads * r.head_dim * elem_bytes;
-  const bool apart = a.prefix > 0 && rows_of(a, false) < kTileRows && (r.n_seqs - 1) * pre > 60e6;
+  const bool apart = a.prefix > 0 && rows_of(a, false) < (elem_bytes == 2 ? kTileRows : 16) &&
+                     (r.n_seqs - 1) * pre > 60e6 + 56.0 * r.n_rows * r.n_q_heads * r.head_dim;
   const long first = apart ? a.prefix : 0;
   auto pick = [&](bool shared, long keys) {
     const bool tile = tiled(a, shared, first, elem_bytes);

@@ -195,7 +195,7 @@ def test_pairs_behind_a_prefix(ops):
     keys[5] = 900
     c = Case(rows, keys, (32, 8, 64), F32, seed=4, shared=912, extra_rows=2)
     c.table[5, :57] = c.table[0, :57]
-    reach(c, B.RT_A_ROWS_PAIRS, prefix=912, prefix_splits=True)
+    reach(c, B.RT_A_ROWS_PAIRS, prefix=912)         # (sixteen rows fill blocks: no pass of the prefix's own)
     compare(ops, c, prefix=912)
 
 
@@ -234,7 +234,7 @@ def shared_case(heads, dtype, seqs, each, prefix, **kw):
     ((16, 8, 128), BF, 64, 1, 1600, B.RT_A_PREFIX_TILES, 1, 8192),
     ((16, 8, 64), BF, 64, 1, 1600, B.RT_A_PREFIX_TILES, 1, 8192),
     ((8, 4, 128), F32, 30, 2, 2080, B.RT_A_ROWS, 0, None),
-    ((32, 8, 128), BF, 32, 20, 640, B.RT_A_TILES, 0, 4096)], ids=repr)
+    ((32, 8, 128), BF, 24, 20, 1920, B.RT_A_TILES, 0, 8192)], ids=repr)
 @pytest.mark.parametrize("value", [math.nan, math.inf])
 def test_prefix_pass_and_values_that_are_not_finite(ops, heads, dtype, seqs, each, prefix, kernel, streamed, max_kv, value):
     c = shared_case(heads, dtype, seqs, each, prefix, fill=value, max_pages=max_kv and max_kv // 16)
@@ -252,7 +252,7 @@ def test_prefix_pass_and_values_that_are_not_finite(ops, heads, dtype, seqs, eac
 @gpu
 @pytest.mark.parametrize("heads,seqs,each,prefix,kernel,max_kv", [
     ((16, 8, 128), 40, 1, 1600, B.RT_A_PREFIX_TILES, None), ((16, 8, 64), 60, 1, 2096, B.RT_A_PREFIX_TILES, None),
-    ((32, 8, 128), 32, 20, 640, B.RT_A_TILES, 4096)], ids=repr)
+    ((32, 8, 128), 24, 20, 1920, B.RT_A_TILES, 8192)], ids=repr)
 def test_prefix_pass_and_pages_outside_the_pool(ops, heads, seqs, each, prefix, kernel, max_kv):
     c = shared_case(heads, BF, seqs, each, prefix, max_pages=max_kv and max_kv // 16)
     c.table[:, 3], c.table[:, prefix // 16 - 1] = -1, c.n_pages + 5

@@ -86,6 +86,20 @@ def test_steps_that_nobody_counted_are_steps(max_rows):
     assert choose(B.RT_A_STREAMED, (40, 8, 128), B.RT_BF16, 64, 64, **kw) == 1
 
 
+@pytest.mark.parametrize("n_seqs,prefix,taken", [(16, 1024, False), (32, 1024, False), (64, 1024, False), (16, 2048, True),
+                                                 (32, 2048, True), (16, 4096, True), (4, 4096, False)])
+def test_blocks_behind_a_prefix_weigh_the_parts_too(n_seqs, prefix, taken):
+    splits = choose(B.RT_A_PREFIX_SPLITS, (32, 8, 128), B.RT_BF16, n_seqs, 16 * n_seqs, max_kv=prefix + 116, prefix=prefix)
+    assert (splits > 0) == taken
+
+
+@pytest.mark.parametrize("rows,taken", [(1, True), (3, True), (4, False), (16, False)])
+def test_blocks_that_rows_fill_gain_nothing_in_fp32(rows, taken):
+    """Four query heads a KV head: four rows fill a block of 16."""
+    splits = choose(B.RT_A_PREFIX_SPLITS, (32, 8, 64), B.RT_F32, 64, 64 * rows, max_kv=4300, prefix=4096)
+    assert (splits > 0) == taken
+
+
 def step_prefix(name, seqs, prefix, positions):
     wl = get(name, batch=seqs, prompt_len=(positions, positions), new_tokens=40)
     cfg = config_from(wl.target, dtype=wl.dtype, draft_layers=wl.draft_layers, cond_layers=wl.cond_layers,
