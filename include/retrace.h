@@ -478,9 +478,8 @@ enum {
 enum {
   RT_A_ROWS = 1,           /* blocks of 16 (token, head) rows */
   RT_A_ROWS_PAIRS = 2,     /* two such blocks a workgroup */
-  RT_A_TILES = 3,          /* tiles of 128 rows, two LDS stages */
-  RT_A_TILES_DEEP = 4,     /* and four */
-  RT_A_PREFIX_TILES = 5    /* the prefix in tiles, the sequences' own keys in blocks of 16 rows */
+  RT_A_TILES = 3,          /* tiles of 128 rows */
+  RT_A_PREFIX_TILES = 4    /* the prefix in tiles, the sequences' own keys in blocks of 16 rows */
 };
 int rt_debug_attn_choice(const rt_paged_kv* kv, const rt_attn_args* args, int32_t choice);
 

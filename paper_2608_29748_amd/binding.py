@@ -42,7 +42,7 @@ KERNEL_KIND_NAMES = ["gemm_qkv", "gemm_o", "gemm_gate_up", "gemm_down", "gemm_co
                      "attention", "attn_merge", "rmsnorm", "qkv_post", "lm_head", "misc"]
 RT_C_ATTN_SLOTS, RT_C_PAGE_POST, RT_C_PROMPT_ROWS, RT_C_GEMM_COLS, RT_C_STEP_PREFIX = range(5)
 RT_A_KERNEL, RT_A_STREAMED, RT_A_SPLITS, RT_A_PREFIX_SPLITS = range(4)
-RT_A_ROWS, RT_A_ROWS_PAIRS, RT_A_TILES, RT_A_TILES_DEEP, RT_A_PREFIX_TILES = range(1, 6)
+RT_A_ROWS, RT_A_ROWS_PAIRS, RT_A_TILES, RT_A_PREFIX_TILES = range(1, 5)
 STAGE_NAMES = ["condition", "draft", "draft_lm_head", "verify", "verify_lm_head", "accept", "context_append"]
 RT_PROF_STAGES = 7
 

@@ -414,7 +414,7 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, const PagedPas
 // Tile kernel (bf16, many rows per page): one workgroup of four waves per block of 128 (token,
 // head) rows, KV head and key split.  A wave owns 32 rows, one per column of 32x32x16 MFMAs; chunks of
 // 64 keys (four pages of K, four of V, one of each copied by every wave straight into LDS) pass
-// through NST LDS stages, the copies of the next chunks in flight while one is used, one barrier a
+// through two LDS stages, the copies of the next chunk in flight while one is used, one barrier a
 // chunk.  S^T = K Q^T with the K rows of a page taken in the order that swaps bits 2 and 3 of the
 // row, so that a lane's eight scores of a page belong to eight consecutive keys, which is the
 // B operand of O^T = V^T P^T as it stands, and V^T's fragments are contiguous 1 KiB reads.  K rows
@@ -425,6 +425,8 @@ __device__ __forceinline__ void rows_body(const PagedAttnArgs& a, const PagedPas
 // prompt of 16384 tokens with a window of 4096, 32 heads of 128 (963 GFLOP, half as many again with the second
 // part), takes 1.33 ms (725 TFLOP/s; 1.09 PFLOP/s of matrix instructions), with one part 1.01.  Head_dim 64 keeps
 // three workgroups a compute unit for 16 bytes of scratch (8192 tokens, window 2048: 221 us, with two 236).
+// Four stages were no faster where a workgroup has a compute unit to itself (32 heads over 8 of 128: 16 rows over
+// 16400 keys 27.5 us, with four 29.6; 64 over 2000 19.7, 20.7; 128 over 8000 42.4, 42.3).
 constexpr int kTileRows = 128;
 constexpr int kChunkT = 64;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
@@ -441,19 +443,18 @@ __device__ __forceinline__ void copy_page(const char* src, char* dst, const int*
     __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (lds_void_t*)(dst + j * 1024), 16, off[j], j * step, 0, 0);
 }
 
-template <int HD, int NST>
+template <int HD>
 struct TileLds {
-  char stage[NST * 2 * (kChunkT / kPage) * kPage * HD * 2];
+  char stage[2 * 2 * (kChunkT / kPage) * kPage * HD * 2];
 };
-template <int HD, int NST>
-__device__ __forceinline__ void tile_body(const PagedAttnArgs& a, const PagedPass& ps, int group, TileLds<HD, NST>& lds) {
+template <int HD>
+__device__ __forceinline__ void tile_body(const PagedAttnArgs& a, const PagedPass& ps, int group, TileLds<HD>& lds) {
   constexpr int ROWB = HD * 2, NP = ROWB / 16, PGB = kPage * ROWB, NLD = PGB / 1024;
   constexpr int PAGES = kChunkT / kPage, STG = 2 * PAGES * PGB;
   constexpr int NKS = HD / 16, NDT = HD / 32;
   constexpr int OPB = ROWB + 16;                       // pitch of a finished row in LDS
   static_assert(2 * STG >= kTileRows * OPB, "finished rows fit the stages");
-  static_assert(NST == 2 || NST == 4, "stage offsets wrap by a mask");
-  static_assert(sizeof(lds.stage) == NST * STG, "stages");
+  static_assert(sizeof(lds.stage) == 2 * STG, "stages");
   char* const smem = lds.stage;
   const PagedRows& r = a.r;
   const int lane = threadIdx.x & 63, g = lane >> 5, c32 = lane & 31;
@@ -505,17 +506,13 @@ __device__ __forceinline__ void tile_body(const PagedAttnArgs& a, const PagedPas
     copy_page<NLD>((const char*)r.k + at, l, koff, 0);
     copy_page<NLD>((const char*)r.v + at, l + PAGES * PGB, voff, 1024);
   };
-  // page ids of the chunk in use and of the next NST: the last are asked for at the end of a step
+  // page ids of the chunk in use and of the next two: the last are asked for at the end of a step
   // (a scalar load under way would make every LDS wait a full one)
-  Pages ids[NST + 1];
-#pragma unroll
-  for (int x = 0; x <= NST; ++x) ids[x] = Pages{};
+  Pages ids[3] = {};
   if (i_beg < i_end) {
 #pragma unroll
-    for (int x = 0; x <= NST; ++x) ids[x] = pages_at(min(i_beg + x, i_end - 1));
-#pragma unroll
-    for (int x = 0; x < NST - 1; ++x)
-      if (i_beg + x < i_end) issue(ids[x], x * STG);
+    for (int x = 0; x < 3; ++x) ids[x] = pages_at(min(i_beg + x, i_end - 1));
+    issue(ids[0], 0);
   }
   // this lane's row
   const int wrow = row0 + w * 32;
@@ -548,19 +545,16 @@ __device__ __forceinline__ void tile_body(const PagedAttnArgs& a, const PagedPas
 
   int stage = 0;
   for (int i = i_beg; i < i_end; ++i) {
-    // this wave's copies of chunk i have landed, those of later ones may be under way
-    if (NST == 4 && i + 2 < i_end) wait_vm<(NST - 2) * 2 * NLD>();
-    else if (NST == 4 && i + 1 < i_end) wait_vm<2 * NLD>();
-    else wait_vm<0>();
+    wait_vm<0>();      // this wave's copies of chunk i have landed
     lds_barrier();     // everyone's have; chunk i-1's stage is free
     const Pages here = ids[0];
-    if (i + NST - 1 < i_end) issue(ids[NST - 1], (stage + (NST - 1) * STG) & (NST * STG - 1));
-#pragma unroll
-    for (int x = 0; x < NST; ++x) ids[x] = ids[x + 1];
-    auto next_pages = [&]() { ids[NST] = pages_at(min(i + NST + 1, i_end - 1)); };
+    if (i + 1 < i_end) issue(ids[1], stage ^ STG);
+    ids[0] = ids[1];
+    ids[1] = ids[2];
+    auto next_pages = [&]() { ids[2] = pages_at(min(i + 3, i_end - 1)); };
     const int k0 = st.key(i);
     const char* sm = smem + stage;
-    stage = (stage + STG) & (NST * STG - 1);
+    stage ^= STG;
     // (a wave none of whose rows sees the chunk passes it by)
     if (!live || !((k0 < max_hi && k0 + kChunkT > min_lo) || k0 < max_snk)) {
       next_pages();
@@ -770,12 +764,11 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_rows_kernel(PagedAttnArgs a,
   const bool first = (int)blockIdx.x < p0.groups;
   rows_body<T, HD, NT, NW, NTL>(a, first ? p0 : p1, blockIdx.x - (first ? 0 : p0.groups), lds);
 }
-template <int HD, int NST>
-__global__ __launch_bounds__(256, NST > 2 ? 1 : HD == 64 ? 3 : 2) void paged_tile_kernel(PagedAttnArgs a, PagedPass p0,
-                                                                                       PagedPass p1) {
-  __shared__ __attribute__((aligned(1024))) TileLds<HD, NST> lds;
+template <int HD>
+__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void paged_tile_kernel(PagedAttnArgs a, PagedPass p0, PagedPass p1) {
+  __shared__ __attribute__((aligned(1024))) TileLds<HD> lds;
   const bool first = (int)blockIdx.x < p0.groups;
-  tile_body<HD, NST>(a, first ? p0 : p1, blockIdx.x - (first ? 0 : p0.groups), lds);
+  tile_body<HD>(a, first ? p0 : p1, blockIdx.x - (first ? 0 : p0.groups), lds);
 }
 // The prefix in tiles, the sequences' own keys by rows: the first is bound by arithmetic, the second
 // by memory, and a compute unit runs one of each (64 tokens behind 8192 shared and up to 1024 own keys: 48 us with
@@ -783,11 +776,11 @@ __global__ __launch_bounds__(256, NST > 2 ? 1 : HD == 64 ? 3 : 2) void paged_til
 template <int HD, bool NTL>
 __global__ __launch_bounds__(256, 2) void paged_both_kernel(PagedAttnArgs a, PagedPass p0, PagedPass p1) {
   union Lds {
-    TileLds<HD, 2> t;
+    TileLds<HD> t;
     RowsLds<HD, 1, 4> r;
   };
   __shared__ __attribute__((aligned(1024))) char lds[sizeof(Lds)];
-  if ((int)blockIdx.x < p0.groups) tile_body<HD, 2>(a, p0, blockIdx.x, reinterpret_cast<Lds*>(lds)->t);
+  if ((int)blockIdx.x < p0.groups) tile_body<HD>(a, p0, blockIdx.x, reinterpret_cast<Lds*>(lds)->t);
   else rows_body<bf16_t, HD, 1, 4, NTL>(a, p1, blockIdx.x - p0.groups, reinterpret_cast<Lds*>(lds)->r);
 }
 
@@ -962,9 +955,8 @@ PagedChoice paged_choice(const PagedAttnArgs& a, const PagedPlan& p, int elem_by
   PagedChoice c{};
   c.g0 = p.shared ? row_blocks(a, true, block_size(a, true, first, elem_bytes)) * p.shared * a.r.n_kv_heads : 0;
   c.g1 = row_blocks(a, false, block_size(a, false, first, elem_bytes)) * p.splits * a.r.n_kv_heads;
-  // (own rows in tiles: more than 16 rows of a sequence, the prefix is in tiles too; a workgroup that
-  // has a compute unit to itself takes twice the stages)
-  c.kernel = tiled(a, false, first, elem_bytes)              ? c.g0 + c.g1 <= 256 ? RT_A_TILES_DEEP : RT_A_TILES
+  // (own rows in tiles: more than 16 rows of a sequence, the prefix is in tiles too)
+  c.kernel = tiled(a, false, first, elem_bytes)              ? RT_A_TILES
              : p.shared && tiled(a, true, first, elem_bytes) ? RT_A_PREFIX_TILES
              : rows_nt(a, elem_bytes) == 2                   ? RT_A_ROWS_PAIRS
                                                              : RT_A_ROWS;
@@ -987,8 +979,7 @@ static hipError_t launch_hd(const PagedAttnArgs& a, const PagedPlan& p, int i, h
   const PagedPass p1{0, p.shared ? a.prefix : 0, p.splits, p.parts() ? p.shared : -1, (int)c.g1};
   const dim3 gd((unsigned)(c.g0 + c.g1));
   if constexpr (sizeof(T) == 2) {
-    if (c.kernel == RT_A_TILES_DEEP) RT_LAUNCH((paged_tile_kernel<HD, 4>), gd, dim3(256), 0, s, a, p0, p1);
-    else if (c.kernel == RT_A_TILES) RT_LAUNCH((paged_tile_kernel<HD, 2>), gd, dim3(256), 0, s, a, p0, p1);
+    if (c.kernel == RT_A_TILES) RT_LAUNCH((paged_tile_kernel<HD>), gd, dim3(256), 0, s, a, p0, p1);
     else if (c.kernel == RT_A_PREFIX_TILES && c.streamed) RT_LAUNCH((paged_both_kernel<HD, true>), gd, dim3(256), 0, s, a, p0, p1);
     else if (c.kernel == RT_A_PREFIX_TILES) RT_LAUNCH((paged_both_kernel<HD, false>), gd, dim3(256), 0, s, a, p0, p1);
     if (c.kernel != RT_A_ROWS) return hipGetLastError();

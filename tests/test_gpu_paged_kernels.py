@@ -85,7 +85,7 @@ def junk(c, window, sinks, value):
     return c
 
 
-# 128-row tiles over two stages of 64 keys: more than 40e6 places read by blocks of 16 rows
+# 128-row tiles over chunks of 64 keys: more than 40e6 places read by blocks of 16 rows
 TILES = [((32, 8, 128), [700, 1, 0, 650, 617], [790, 300, 40, 650, 680]), ((32, 16, 64), [1310, 1, 0, 1330, 1290], [1400, 300, 40, 1330, 1350])]
 
 
@@ -151,11 +151,11 @@ def test_tiles_in_key_splits(ops, heads):
 @gpu
 @pytest.mark.parametrize("heads,rows", [((32, 8, 128), [500, 12]), ((64, 16, 64), [430, 12])], ids=repr)
 @pytest.mark.parametrize("window,sinks", [(360, 0), (350, 65), (0, 0)])
-def test_deep_tiles(ops, heads, rows, window, sinks):
-    """Four stages, where a workgroup has a compute unit to itself."""
+def test_tiles_of_a_few_workgroups(ops, heads, rows, window, sinks):
+    """A workgroup or less a compute unit, and rows at positions below 0, which see nothing."""
     c = Case(rows, [490, 12 + 300], heads, BF, seed=window, extra_rows=2)
     kw = dict(max_kv=490)
-    reach(c, B.RT_A_TILES_DEEP, window=window, sinks=sinks, **kw)
+    reach(c, B.RT_A_TILES, window=window, sinks=sinks, **kw)
     compare(ops, c, window, sinks, **kw)
 
 

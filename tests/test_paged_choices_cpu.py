@@ -26,7 +26,7 @@ def test_choices_are_checked():
 
 @pytest.mark.parametrize("heads,dtype,n_seqs,rows,kv,kernel", [
     ((32, 8, 128), B.RT_BF16, 16, 16, 300, B.RT_A_ROWS), ((32, 8, 128), B.RT_BF16, 32, 16, 700, B.RT_A_TILES),
-    ((32, 8, 128), B.RT_BF16, 1, 500, 490, B.RT_A_TILES_DEEP), ((32, 8, 128), B.RT_BF16, 1, 16384, 16384, B.RT_A_TILES),
+    ((32, 8, 128), B.RT_BF16, 1, 500, 490, B.RT_A_TILES), ((32, 8, 128), B.RT_BF16, 1, 16384, 16384, B.RT_A_TILES),
     ((32, 8, 128), B.RT_BF16, 64, 1, 16384, B.RT_A_ROWS), ((32, 8, 128), B.RT_F32, 4, 4096, 4096, B.RT_A_ROWS),
     ((32, 8, 64), B.RT_F32, 64, 16, 2000, B.RT_A_ROWS_PAIRS), ((32, 8, 64), B.RT_F32, 4, 16, 2000, B.RT_A_ROWS)], ids=repr)
 def test_kernels(heads, dtype, n_seqs, rows, kv, kernel):
