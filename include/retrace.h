@@ -160,7 +160,8 @@ int rt_prefill_prefix(rt_model* m, int32_t prefix_len, const int32_t* prefix_ids
 /* Gives the target's attention a sliding window with sinks, in every layer: a row sees the last
  * `window` positions, its own included, and the first `sinks` ones (rt_window_attention).  window 0
  * (with sinks 0; the initial state): every position.  The drafter's attention keeps its full context.
- * Holds for the prompts too, so the next call must be a prefill (RT_ERR_STATE otherwise). */
+ * Holds for the prompts too, so the next call must be a prefill (RT_ERR_STATE otherwise).  A graph into
+ * which the caller captured rounds (rt_spec_round_static) keeps the window of its capture. */
 int rt_set_window(rt_model* m, int32_t window, int32_t sinks);
 
 /* One ReTrace round for every prefilled sequence.  Outputs (host):
@@ -250,7 +251,7 @@ typedef struct rt_paged_kv {
  * with the factors of the row's position from `rope`, fp32 [cos, sin][rope_positions][rot_dim / 2]
  * (NULL: no rotation).  Everything is computed in fp32 and rounded once.
  * Rows at positions below 0 or past the page table are skipped, their queries too.  Two rows for
- * one place of the cache leave either there.  q may be NULL (no queries); q_out may be q itself
+ * one place of the cache leave every element of it from one or the other.  q may be NULL (no queries); q_out may be q itself
  * where the dtypes and strides agree, and overlaps the inputs in no other way. */
 typedef struct rt_append_args {
   const void* q;

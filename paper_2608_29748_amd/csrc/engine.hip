@@ -443,9 +443,9 @@ struct Engine : EngineBase {
 
   // Whether a layer's attention is the paged operators': with a window, or in a target-only step where a
   // pass of its own over the shared prefix pays (0.6B shape, 16 sequences behind 8192 positions: a step 3.48
-  // ms with caches apart, 1.44).  Rounds keep their own kernels, which find the shared pages in
-  // the caches (the same batch: a round 5.04 ms apart, 3.98 shared, 4.35 with the operators).  Then their
-  // arguments and plan.
+  // ms with caches apart, 1.47).  Rounds keep their own kernels, which find the shared pages in the caches (the
+  // same batch: a round 5.07 ms apart, 4.11 shared; with the operators it was 4.35 against 3.98, when their tiles still
+  // took one product a weight).  Then their arguments and plan.
   bool paged_layer(const LayerCtx& c, PagedAttnArgs* out, PagedPlan* plan) const {
     const Plan& q = p;
     if (c.window <= 0 && c.prefix <= 0) return false;

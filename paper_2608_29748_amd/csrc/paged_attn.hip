@@ -110,7 +110,7 @@ struct Finite {
 };
 // Sequence and row block of block blk, of `per` (token, head) rows each; false: none.  A sequence's
 // last rows come first: they see the most keys, and short blocks fill the end of a launch (causal prompts, 32 heads
-// over 8 of 128: 4096 tokens 200 -> 180 us, 4 of 2048 214 -> 195).  The results are the same for every lane and
+// over 8 of 128: 4096 tokens 243 -> 219 us, 4 of 2048 247 -> 231).  The results are the same for every lane and
 // made scalar, so that page ids come by scalar loads.
 __device__ __forceinline__ bool block_rows(const PagedAttnArgs& a, bool shared, int blk, int per, int& s, int& rb,
                                            SeqRows& sr) {
@@ -871,9 +871,10 @@ static int rows_nt(const PagedAttnArgs& a, int elem_bytes) {
 // Whether a pass (the sequences' own: from key `first` on) takes the tile kernel: bf16 rows that on the average
 // fill more than one block of 16 and, of the own pass, whose blocks would read more than 160 MB of
 // pages between them (40e6 places of K and V).  Below that the rows kernel, whose waves share a block's
-// keys, ends sooner.  32 heads over 8 of 128, blocks of 16 tokens, rows against tiles: 4 sequences behind 300
-// keys (5e6) 8.2 us, 15.3; 16 behind 300 (21e6) 12.1, 16.5; 4 behind 2048 (34e6) 19.6, 21.6; 8 behind 2048
-// (68e6) 29.3, 24.7; 32 behind 2048 92.8, 66.5.
+// keys, ends sooner.  Rows against tiles, us, 32 heads over 8 of 128: blocks of 16 tokens, 16 sequences behind 300
+// keys (21e6) 11.6, 15.3; 32 (41e6) 20.9, 17.7; 4 behind 2048 (34e6) 20.0, 19.1; 8 (68e6) 30.6, 27.0; 16 behind 1024
+// (68e6) 26.4, 27.8; prompts of 200 tokens, two (20e6) 11.5, 12.8; four (41e6) 19.1, 13.5; of 500, one (64e6) 18.9,
+// 20.2; two 33.1, 21.2.  Heads of 64: 16 tokens, 32 behind 1024 (68e6) 25.0, 31.0; four prompts of 500 31.3, 22.7.
 static bool tiled(const PagedAttnArgs& a, bool shared, long first, int elem_bytes) {
   const PagedRows& r = a.r;
   if (elem_bytes != 2 || rows_of(a, shared) <= 16) return false;
@@ -922,7 +923,8 @@ PagedPlan paged_plan(const PagedAttnArgs& a, int elem_bytes) {
     long most = keys / (tile ? 4 * kChunkT : 8 * kStep);
     if (shared && tile) {
       // Over the prefix a part is written and read for every row of the batch, 0.3 us per 2^17 elements,
-      // while a split takes 1.3 us a chunk: the sum of both is least at the root below; up to the time that
+      // while a split takes 1.3 us a chunk (64 tokens of 32 heads behind 8192 keys: 38.5 us; reckoned with 1.0 39.7,
+      // with 1.7 42.7): the sum of both is least at the root below; up to the time that
       // the sequences' own keys take beside it a split costs nothing.
       const double part = 0.3 / (1 << 17) * r.n_rows * r.n_q_heads * r.head_dim;
       const double own = 1e-6 / 5 * r.n_seqs * keys_of(a, first, a.max_rows) * r.n_kv_heads * r.head_dim * elem_bytes;

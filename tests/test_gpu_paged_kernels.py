@@ -273,6 +273,19 @@ def test_one_prompt_among_tokens_behind_a_prefix(ops, heads, dtype, max_rows):
     compare(ops, c, 300, 4, max_rows=max_rows)
 
 
+@gpu
+@pytest.mark.parametrize("heads,dtype,kernel", [((71, 1, 64), BF, B.RT_A_TILES), ((71, 1, 64), F32, B.RT_A_ROWS),
+                                                ((96, 1, 128), BF, B.RT_A_TILES), ((96, 1, 128), F32, B.RT_A_ROWS)], ids=repr)
+def test_many_heads_of_one(ops, heads, dtype, kernel):
+    """More query heads of a KV head than a block or, with few rows, a tile has rows."""
+    for rows, keys in (([1, 1, 0, 2], [300, 77, 5, 2]), ([900, 3, 0, 1], [950, 3, 9, 400])):
+        c = Case(rows, keys, heads, dtype, seed=9, extra_rows=1)
+        if rows[0] > 1:
+            reach(c, kernel, window=150, sinks=2, max_kv=1000)
+        compare(ops, c, 150, 2)
+        compare(ops, c)
+
+
 def test_the_comparison_sees_what_is_missing():
     """On the host: NaN that should be there and is not, NaN that should not, a number out of bounds."""
     ref, tol = torch.zeros(4, 2, 3, dtype=torch.float64), torch.full((4, 2, 3), 0.1, dtype=torch.float64)
