@@ -287,7 +287,8 @@ int rt_kv_append(const rt_paged_kv* kv, const rt_append_args* args, void* hip_st
  * 0 .. prefix_len - 1 (a multiple of 16; 0: none) lie in the same pages for every sequence, and are
  * found through the first sequence's page table.  A pass of their own reads them once for the whole batch
  * where that pays: where the sequences have fewer than 128 (row, query head) pairs (fp32: 16) for a KV head on the
- * average and reading the prefix once for each would move over 60 MB more, and 56 bytes more for every element of out.
+ * average and reading the prefix once for each would move over 60 MB more, and 56 bytes more
+ * for every element of out.
  *
  * max_rows and max_kv: the most rows and keys of a sequence, as far as the host knows (0: unknown).
  * They only size the split of the work: they must be the same for the call and for its workspace,
@@ -462,11 +463,11 @@ enum {
   RT_C_ATTN_SLOTS = 0,     /* workgroups per KV head of the attention */
   RT_C_PAGE_POST = 1,      /* 1: q|k|v post-processing by KV page, 0: by row (where attention does not do it) */
   RT_C_PROMPT_ROWS = 2,    /* rows per pass of a prefill of n prompt tokens in all (arg unused) */
-  RT_C_STEP_PREFIX = 4,    /* key splits of the pass that a target-only step of n sequences makes over their arg
-                              shared positions (0: none, the ordinary attention runs) */
-  RT_C_GEMM_COLS = 3       /* columns per workgroup of the target GEMM arg (RT_K_GEMM_QKV .. _DOWN, RT_K_LM_HEAD)
+  RT_C_GEMM_COLS = 3,      /* columns per workgroup of the target GEMM arg (RT_K_GEMM_QKV .. _DOWN, RT_K_LM_HEAD)
                               over n rows of a prompt pass (LM head: a round) on the mid-size kernel; 0 where
                               another kernel runs */
+  RT_C_STEP_PREFIX = 4     /* key splits of the pass that a target-only step of n sequences makes over their arg
+                              shared positions (0: none, the ordinary attention runs) */
 };
 int rt_debug_choice(const rt_config* cfg, int32_t choice, int32_t n, int32_t arg);
 /* The same for a call of rt_window_attention or rt_prefix_attention, from its counts alone. */
